@@ -13,6 +13,7 @@
  *   nova_restore_from_cache     Eq. 15-16  fill pruned rows from the residual cache
  *   nova_pruned_scale_forward   all of these for the layers of a scale in one call
  *   nova_*_device               the same steps with the keep counts left on the device
+ *   nova_cache4_*               a K/V cache held in 4 bits: append, read, attention, weights, eviction
  *
  * General rules
  *  - Plain C ABI. No call throws, aborts or traps the GPU. Every call returns a
@@ -547,6 +548,74 @@ nova_status nova_restore_from_cache_device(nova_ctx* ctx, const void* x_in, cons
                                            const int32_t* cu_keep, const void* cache_prev,
                                            int hp, int wp, int h, int w, int C, int B,
                                            void* x_out, void* cache_out, void* stream);
+
+/* ---- a K/V cache held in 4 bits ------------------------------------------------------------------- */
+/*
+ * (No counterpart in the paper, which keeps every kept token's keys and values of every scale in bf16 to the end of the
+ * generation.) The calls below fill, read and shorten a cache of one layer that takes 4.5 bits a channel instead of 16.
+ * Format: a row of C channels is C/2 bytes of codes and C/32 bf16 scales. Each group of 32 channels has one scale s, its
+ * largest magnitude divided by 7 and rounded up to five significant bits; a channel is round(x / s), to nearest with ties to
+ * even, a whole number from -7 to 7, and stands for that number times s, which bf16 holds exactly. Codes are stored plus 8, eight
+ * channels c..c+7 in a little-endian 32-bit word: channel c+2i in bits 4i..4i+3, channel c+2i+1 in bits 16+4i..19+4i.
+ * A group that holds a NaN, an infinity or a magnitude of 2^120 or more gets scale NaN (its channels read as NaN; the
+ * device status is NOVA_ERR_NONFINITE); no scale is below 2^-120 except that of zeros, which is 0.
+ * C a multiple of 64, head size 64 or 128, as many K/V heads as query heads. Rows at or past kv_len[b] are never read and may
+ * hold anything. Calls that take compacted rows get them as nova_select_topk writes them: image b's are cu[b] .. cu[b+1]-1 of
+ * M (an upper bound of cu[B]; rows past cu[B] are neither read nor written), with a row stride of ld elements (ld >= C, a
+ * multiple of 8). In debug mode cu is validated on the device first.
+ */
+typedef struct nova_cache4 {
+    void *k_codes, *v_codes;       /* device uint8 [B, Lmax, C/2]  */
+    void *k_scales, *v_scales;     /* device bf16 [B, Lmax, C/32]  */
+    int32_t* kv_len;               /* device int32 [B]             */
+    int B, Lmax, C, n_heads;
+} nova_cache4;
+
+/* Bytes of workspace (nova_set_workspace) with which every call below runs on this cache for up to M rows; 0 on bad sizes. */
+size_t      nova_cache4_workspace_bytes(const nova_ctx* ctx, const nova_cache4* c, int M);
+
+/*
+ * Rounds the rows of k and v (device bf16 [M, C], both with row stride ld) to 4 bits and writes image b's to cache rows kv_len[b] ...
+ * With advance != 0 kv_len[b] then grows by cu_rows[b+1] - cu_rows[b]. An image whose rows do not fit in Lmax
+ * records NOVA_ERR_SHAPE in the device status word; its rows are not written and its length stays.
+ * nova_cache4_read is the way back: cache rows first[b] .. first[b] + cu_rows[b+1] - cu_rows[b] - 1 (first device int32 [B], NULL = 0)
+ * as bf16 to k_out and v_out. A row outside [0, Lmax) records NOVA_ERR_SHAPE and is not written.
+ */
+nova_status nova_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* k, const void* v, int64_t ld,
+                               const int32_t* cu_rows, int M, int advance, void* stream);
+nova_status nova_cache4_read(nova_ctx* ctx, const nova_cache4* c, const int32_t* first, const int32_t* cu_rows, int M,
+                             void* k_out, void* v_out, int64_t ld, void* stream);
+
+/*
+ * o = softmax(q K^T / sqrt(dh)) V per head, without mask: the queries of image b attend to its rows [0, kv_len[b]).
+ * q device bf16 [M, C] with row stride ldq; o device bf16 [M, C] contiguous; lse device f32 [n_heads, M] or NULL: the natural
+ * logarithm of the sum of the exponentials of the scores. Queries of an image without rows get o = 0 and lse = -inf.
+ * Products of bf16 operands with fp32 accumulation, probabilities rounded to bf16 for the product with V. The order of the sums
+ * follows from the sizes, the counts and the SM count.
+ */
+nova_status nova_cache4_attention(nova_ctx* ctx, const nova_cache4* c, const void* q, int64_t ldq, const int32_t* cu_q, int M,
+                                  void* o, float* lse, void* stream);
+
+/*
+ * weight_out[b, j] = weight_in[b, j] + sum over heads and image b's queries of exp(q k_j / sqrt(dh) - lse), for the rows
+ * j < kv_len[b] of the cache: the attention weight a row has received, over the calls made so far if weight_in is what the
+ * last one wrote. weight_in, weight_out device f32 [B, Lmax]; weight_in may be NULL (zeros) or weight_out itself; entries at or past
+ * kv_len[b] are not written. q and lse as given to and left by nova_cache4_attention; a query with lse = -inf counts for nothing.
+ */
+nova_status nova_cache4_weights(nova_ctx* ctx, const nova_cache4* c, const void* q, int64_t ldq, const float* lse,
+                                const int32_t* cu_q, int M, const float* weight_in, float* weight_out, void* stream);
+
+/*
+ * Eviction into another cache of the same images, width and heads (no memory shared; budget <= dst->Lmax). Of an image with more than
+ * `budget` rows the last `recent` stay (recent <= budget) and, of those before them, the budget - recent with the highest weight,
+ * ties to the lower row; of the others all rows. They keep their order. Written: dst's rows and kv_len; weight_out (device f32
+ * [B, dst->Lmax] or NULL): the weights of the rows that stayed, then zeros, so that rows appended later start from nothing;
+ * src_row (device int32 [B, budget] or NULL): the old row of each new one, then -1 (with NULL the list takes B * budget * 4 bytes of the
+ * workspace). weight device f32 [B, Lmax]: entries below kv_len[b] must not be NaN. c itself is left as it is.
+ * Errors: budget > dst->Lmax -> SHAPE; shared memory between the two caches or the weights -> INVALID_ARG.
+ */
+nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* weight, int budget, int recent,
+                              const nova_cache4* dst, float* weight_out, int32_t* src_row, void* stream);
 
 #ifdef __cplusplus
 }

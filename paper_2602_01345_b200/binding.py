@@ -190,6 +190,12 @@ class Context:
         if self._workspace is None or self._workspace.numel() < need:
             self.set_workspace(torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{self.device}"))
 
+    def ensure_cache4_workspace(self, cache: "Cache4", rows: int):
+        """A workspace with which every nova_cache4 call runs on this cache for up to `rows` rows."""
+        need = nova_cache4_workspace_bytes(self, cache, rows)
+        if self._workspace is None or self._workspace.numel() < need:
+            self.set_workspace(torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{self.device}"))
+
     def set_wait_limit_ns(self, ns: int):
         """Limit of every device-side wait of this context's later launches (0 = default, 1 s)."""
         _lib.nova_set_wait_limit_ns.argtypes = [_vp, C.c_ulonglong]
@@ -719,3 +725,126 @@ class ScaleCall:
                                                           C.byref(cs), t, first, count, int(bool(append_kv)), _stream(stream)))
         finally:
             io.scale_logits = None      # of this pass only, whether or not it went through
+
+
+# ---- a K/V cache held in 4 bits -------------------------------------------------------------------------------
+class _Cache4(C.Structure):
+    _fields_ = [(n, _vp) for n in ("k_codes", "v_codes", "k_scales", "v_scales", "kv_len")] + \
+               [(n, _i) for n in ("B", "Lmax", "C", "n_heads")]
+
+
+_lib.nova_cache4_workspace_bytes.argtypes = [_vp, C.POINTER(_Cache4), _i]
+_lib.nova_cache4_workspace_bytes.restype = C.c_size_t
+_lib.nova_cache4_append.argtypes = [_vp, C.POINTER(_Cache4), _vp, _vp, _i64, _vp, _i, _i, _vp]
+_lib.nova_cache4_append.restype = _i
+_lib.nova_cache4_read.argtypes = [_vp, C.POINTER(_Cache4), _vp, _vp, _i, _vp, _vp, _i64, _vp]
+_lib.nova_cache4_read.restype = _i
+_lib.nova_cache4_attention.argtypes = [_vp, C.POINTER(_Cache4), _vp, _i64, _vp, _i, _vp, _vp, _vp]
+_lib.nova_cache4_attention.restype = _i
+_lib.nova_cache4_weights.argtypes = [_vp, C.POINTER(_Cache4), _vp, _i64, _vp, _vp, _i, _vp, _vp, _vp]
+_lib.nova_cache4_weights.restype = _i
+_lib.nova_cache4_evict.argtypes = [_vp, C.POINTER(_Cache4), _vp, _i, _i, C.POINTER(_Cache4), _vp, _vp, _vp]
+_lib.nova_cache4_evict.restype = _i
+
+
+class Cache4:
+    """A layer's K/V cache in 4 bits: the device tensors k_codes, v_codes uint8 [B, Lmax, C/2], k_scales, v_scales bf16
+    [B, Lmax, C/32] and kv_len int32 [B], and the C struct that points to them."""
+
+    def __init__(self, k_codes, v_codes, k_scales, v_scales, kv_len, n_heads: int):
+        B, Lmax, half = k_codes.shape
+        Cc = 2 * half
+        for t in (k_codes, v_codes):
+            assert t.dtype == torch.uint8 and t.shape == (B, Lmax, half) and t.is_contiguous()
+        for t in (k_scales, v_scales):
+            assert t.dtype == torch.bfloat16 and t.shape == (B, Lmax, Cc // 32) and t.is_contiguous()
+        assert kv_len.dtype == torch.int32 and kv_len.shape == (B,) and kv_len.is_contiguous()
+        assert len({t.device for t in (k_codes, v_codes, k_scales, v_scales, kv_len)}) == 1
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.kv_len = k_codes, v_codes, k_scales, v_scales, kv_len
+        self.B, self.Lmax, self.C, self.n_heads = B, Lmax, Cc, int(n_heads)
+        self.c = _Cache4(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), _ptr(kv_len), B, Lmax, Cc, self.n_heads)
+
+    @classmethod
+    def empty(cls, B: int, Lmax: int, C: int, n_heads: int, device="cuda:0"):
+        """A cache without rows. (The rows' memory is not initialised: nothing at or past kv_len is read.)"""
+        def new(width, dtype):
+            return torch.empty((B, Lmax, width), dtype=dtype, device=device)
+        return cls(new(C // 2, torch.uint8), new(C // 2, torch.uint8), new(C // 32, torch.bfloat16), new(C // 32, torch.bfloat16),
+                   torch.zeros((B,), dtype=torch.int32, device=device), n_heads)
+
+
+def _rows4(cache: Cache4, t):
+    """Checks compacted rows [M, C] (rows may lie apart, as slices of a wider tensor do) and gives their row stride."""
+    assert t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[1] == cache.C and t.stride(1) == 1, "rows must be bf16 [M, C]"
+    return t.stride(0) if t.shape[0] > 1 else cache.C
+
+
+def _same_device4(ctx: Context, cache: Cache4, *tensors):
+    for t in (cache.kv_len,) + tensors:
+        assert t is None or (t.is_cuda and t.device.index == ctx.device), "tensors must lie on the context's device"
+
+
+def _cu4(cache: Cache4, cu):
+    assert cu.dtype == torch.int32 and cu.numel() == cache.B + 1, "cu must be int32 [B + 1]"
+    return _ptr(cu)
+
+
+def nova_cache4_workspace_bytes(ctx: Context, cache: Cache4, M: int) -> int:
+    return int(_lib.nova_cache4_workspace_bytes(ctx.handle, C.byref(cache.c), M))
+
+
+def nova_cache4_append(ctx: Context, cache: Cache4, k, v, cu_rows, advance: bool = True, stream=None):
+    """Rounds the rows of k and v (bf16 [M, C], image b's at cu_rows[b] .. cu_rows[b+1]-1) to 4 bits and writes them behind
+    the cache's rows; advance: kv_len then counts them."""
+    M, ld = k.shape[0], _rows4(cache, k)
+    assert v.shape == k.shape and _rows4(cache, v) == ld, "k and v must have one layout"
+    _same_device4(ctx, cache, k, v, cu_rows)
+    ctx.check(_lib.nova_cache4_append(ctx.handle, C.byref(cache.c), k.data_ptr() if M else None, v.data_ptr() if M else None, ld,
+                                      _cu4(cache, cu_rows), M, int(bool(advance)), _stream(stream)))
+
+
+def nova_cache4_read(ctx: Context, cache: Cache4, cu_rows, k_out, v_out, first=None, stream=None):
+    """Cache rows first[b] .. (int32 [B]; None: from row 0), cu_rows[b+1] - cu_rows[b] of them, as bf16 to rows cu_rows[b] .. of
+    k_out and v_out [M, C]."""
+    M, ld = k_out.shape[0], _rows4(cache, k_out)
+    assert v_out.shape == k_out.shape and _rows4(cache, v_out) == ld, "k_out and v_out must have one layout"
+    assert first is None or (first.dtype == torch.int32 and first.numel() == cache.B)
+    _same_device4(ctx, cache, k_out, v_out, cu_rows, first)
+    ctx.check(_lib.nova_cache4_read(ctx.handle, C.byref(cache.c), _ptr(first), _cu4(cache, cu_rows), M, k_out.data_ptr() if M else None,
+                                    v_out.data_ptr() if M else None, ld, _stream(stream)))
+
+
+def nova_cache4_attention(ctx: Context, cache: Cache4, q, cu_q, o, lse=None, stream=None):
+    """o [M, C] bf16 = attention of the queries q [M, C] (image b's at cu_q[b] .. cu_q[b+1]-1) over the cache's rows; lse f32
+    [n_heads, M] or None: the log-sum-exp of every query's scores. Needs a workspace (Context.ensure_cache4_workspace)."""
+    M, ld = q.shape[0], _rows4(cache, q)
+    assert o.dtype == torch.bfloat16 and o.shape == q.shape
+    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (cache.n_heads, M))
+    _same_device4(ctx, cache, q, cu_q, o, lse)
+    ctx.check(_lib.nova_cache4_attention(ctx.handle, C.byref(cache.c), q.data_ptr() if M else None, ld, _cu4(cache, cu_q), M, _ptr(o),
+                                         _ptr(lse), _stream(stream)))
+
+
+def nova_cache4_weights(ctx: Context, cache: Cache4, q, lse, cu_q, weight_out, weight_in=None, stream=None):
+    """weight_out [B, Lmax] f32 = weight_in (None: zeros; may be weight_out itself) + the attention weight that each cached row
+    receives from these queries, given the log-sum-exp that nova_cache4_attention left."""
+    M, ld = q.shape[0], _rows4(cache, q)
+    assert lse.dtype == torch.float32 and lse.shape == (cache.n_heads, M)
+    for t in (weight_in, weight_out):
+        assert t is None or (t.dtype == torch.float32 and t.shape == (cache.B, cache.Lmax))
+    _same_device4(ctx, cache, q, lse, cu_q, weight_out, weight_in)
+    ctx.check(_lib.nova_cache4_weights(ctx.handle, C.byref(cache.c), q.data_ptr() if M else None, ld, _ptr(lse), _cu4(cache, cu_q), M,
+                                       _ptr(weight_in), _ptr(weight_out), _stream(stream)))
+
+
+def nova_cache4_evict(ctx: Context, cache: Cache4, weight, budget: int, recent: int, dst: Cache4, weight_out=None, src_row=None,
+                      stream=None):
+    """Writes to dst the cache's last `recent` rows and the highest-weighted of the others, `budget` in all per image, in their
+    order. weight f32 [B, Lmax]; weight_out f32 [B, dst.Lmax] or None; src_row int32 [B, budget] or None (then the workspace
+    holds the list)."""
+    assert weight.dtype == torch.float32 and weight.shape == (cache.B, cache.Lmax)
+    assert weight_out is None or (weight_out.dtype == torch.float32 and weight_out.shape == (dst.B, dst.Lmax))
+    assert src_row is None or (src_row.dtype == torch.int32 and src_row.shape == (cache.B, budget))
+    _same_device4(ctx, cache, weight, dst.kv_len, weight_out, src_row)
+    ctx.check(_lib.nova_cache4_evict(ctx.handle, C.byref(cache.c), _ptr(weight), budget, recent, C.byref(dst.c), _ptr(weight_out),
+                                     _ptr(src_row), _stream(stream)))

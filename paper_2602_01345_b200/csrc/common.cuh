@@ -28,6 +28,8 @@
 #define NOVA_MEAN_MAX_CTAS 192        // the accumulator's arrival count has 8 bits
 #define NOVA_MEAN_MAX_SEGMENTS 256
 #define NOVA_TICKETS 1024             // of rows that several CTAs share: head, eight for each CTA pair (its reading warps), or attention mass, one for each CTA
+#define NOVA_TICKET_WORD0 (NOVA_STATUS_WORDS + NOVA_MEAN_MAX_SEGMENTS * 2)
+#define NOVA_APPEND_TICKET_WORD 4     // blocks of a cache4 append that have read the lengths
 #define NOVA_STATUS_BYTES (NOVA_STATUS_WORDS * 4 + NOVA_MEAN_MAX_SEGMENTS * 8 + NOVA_TICKETS * 4)
 // Behind it: partial results of such rows. Head: [pair][first or last of its row blocks][m, s, u][256 rows] fp32; attention mass:
 // [CTA, up to two per SM][first or last of its rows][128 rows] float2.
@@ -39,7 +41,7 @@ static_assert(2 * 2 * 128 * 8 >= NOVA_HEAD_SLOT_FLOATS * 4, "two slots for every
 enum nova_kernel_cat {
     NOVA_K_ENTROPY = 0, NOVA_K_ENTROPY_MEAN, NOVA_K_SELECT, NOVA_K_LAYERNORM,
     NOVA_K_GEMM_QKV, NOVA_K_ATTENTION, NOVA_K_GEMM_PROJ, NOVA_K_GEMM_FC1, NOVA_K_GEMM_FC2,
-    NOVA_K_RESTORE, NOVA_K_KEEP_RATIOS, NOVA_K_SCORE, NOVA_K_COUNT
+    NOVA_K_RESTORE, NOVA_K_KEEP_RATIOS, NOVA_K_SCORE, NOVA_K_CACHE4, NOVA_K_COUNT
 };
 
 struct nova_prof_rec {
