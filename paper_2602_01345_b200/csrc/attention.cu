@@ -39,7 +39,7 @@
 // table, loads, S, softmax, O. Measured against the kernel before it (two tiles of one item in a CTA), us:
 // 3277 rows x 29414 keys, 16 heads x 128: 684 -> 572; 4 x 2048 x 8473: 510 -> 416; 1024 x 7449: 86 -> 52;
 // 300 x 821: 22.8 -> 12.5; 4 x 563 x 1779, 30 heads x 64: 80 -> 55; 2 x 128 x 552, 16 x 64: 11.8 -> 9.2.
-#include "tc_common.cuh"
+#include "cache4.cuh"
 
 namespace {
 
@@ -48,7 +48,8 @@ using namespace tc;
 constexpr int BQ = 128;        // query rows per CTA
 constexpr int BKV = 128;       // keys per tile
 constexpr int kBufs = 3;       // S buffers in tensor memory
-constexpr int kThreads = 512;  // warpgroups: producer + issuer (+2 idle warps), epilogue, softmax 0, softmax 1
+constexpr int kThreads512 = 512;  // warpgroups: producer + issuer (+2 idle warps), epilogue, softmax 0, softmax 1
+constexpr int kThreads4 = 640; // and one that decodes keys and values, with a cache in 4 bits
 constexpr int kSlabBytes = 128 * 128;   // [128 rows][64 bf16]
 // The probability of a score equal to the reference is 2^-kHeadroom. A row's sum of probabilities over one key tile at
 // or above kHugeSum (or NaN) means a score about 2^(80 + kHeadroom) above the reference. That is far below
@@ -61,8 +62,9 @@ constexpr float kHugeSum = 1.2089258e24f;   // 2^80
 // waited for the epilogue of the pass before that tile's: passes up to i - kBufs - 3 are done with their slots.
 constexpr int kSlots = kBufs + 3;
 
-template <int DH>
+template <int DH, bool Q4>
 struct AttnCfg {
+    static constexpr int kThreads = Q4 ? kThreads4 : kThreads512;
     static constexpr bool kPair = (DH == 128);
     static constexpr int kCtas = kPair ? 2 : 1;
     static constexpr int kRows = kCtas * BQ;                    // query rows of one work item
@@ -70,14 +72,20 @@ struct AttnCfg {
     static constexpr int kVCols = DH / kCtas;                   // columns of V per CTA (all keys)
     static constexpr int kQBytes = BQ * DH * 2;
     static constexpr int kTileBytes = kKRows * DH * 2;          // K and V alike (BKV * kVCols * 2)
-    static constexpr int kStages = kPair ? 4 : 5;               // stage: K of a tile and V of the tile kBufs before it
+    static constexpr int kStages = Q4 ? 3 : kPair ? 4 : 5;      // stage: K of a tile and V of the tile kBufs before it
     static constexpr int kStageOff = 2 * kQBytes;
     static constexpr int kLOff = kStageOff + kStages * 2 * kTileBytes;  // [kSlots][2][128] row sums of the two warpgroups
     static constexpr int kMOff = kLOff + kSlots * 2 * BQ * 4;           // [kSlots][128] reference maxima
     static constexpr int kAOff = kMOff + kSlots * BQ * 4;               // [2][128] maxima of a maximum pass
     static constexpr int kTabOff = kAOff + 2 * BQ * 4;                  // [kTable] passes
-    static constexpr int kBarOff = kTabOff + 64 * 44;
-    static constexpr int kTotal = kBarOff + 512 + 1024;
+    static constexpr int kBarOff = kTabOff + 64 * 52;
+    // Q4: [kRing][2][128 threads] pieces of 32 bytes of codes (as two planes of 16), and their scales
+    static constexpr int kRing = 5;
+    static constexpr int kRingBytes = 128 * 2 * (32 + 4);
+    static constexpr int kRingOff = kBarOff + 512;
+    static constexpr int kTotal = kBarOff + 512 + 1024 + (Q4 ? kRing * kRingBytes : 0);
+    static_assert(kTotal <= 227 * 1024, "shared memory");
+    static_assert(kKRows * (DH / 64) == 128 && 128 * (kVCols / 64) == 128, "a decoding thread has 64 channels of a key and of a value");
     static_assert(kVCols == 64, "a V stage is one 128-byte-wide slab");
 };
 
@@ -94,6 +102,11 @@ struct AttnParams {
     unsigned int* tickets;
     int part_slots;
     unsigned int* status;
+    // a cache in 4 bits
+    const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+    float* lse;                    // [n_heads, M] or NULL
+    int M;
+    int max_parts;                 // that there is scratch memory for, of a split item
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -143,6 +156,18 @@ __device__ __forceinline__ uint64_t sub_f32x2(uint64_t a, uint64_t b)
     asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float clamp_nan(float x)     // to [-126, 126], NaN stays NaN
+{
+    float r;
+    asm("{\n.reg .f32 t;\nmax.NaN.f32 t, %1, 0fC2FC0000;\nmin.NaN.f32 %0, t, 0f42FC0000;\n}\n" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ float fmax3(float a, float b, float c)
 {
     float r;
@@ -157,21 +182,39 @@ __device__ __forceinline__ float fmax3(float a, float b, float c)
 // probabilities get next) and j is added to the exponent field as an integer. x is clamped to
 // [-126, 126] so that the exponent cannot wrap; a masked (-inf) score therefore yields 2^-126, not 0,
 // and one far above the reference a value that the overflow check sees.
+// FINE: a quartic, 2.6e-6, where the sums are a result of their own (the log-sum-exp), and a NaN stays one (the clamps pass it on, and
+// 2^j is a factor instead of an addition to the exponent field).
+template <bool FINE>
 __device__ __forceinline__ void exp2_poly_x2(uint64_t x2, float& p0, float& p1)
 {
     float x0, x1;
     unpack_f32x2(x2, x0, x1);
-    const uint64_t xc = pack_f32x2(fminf(fmaxf(x0, -126.f), 126.f), fminf(fmaxf(x1, -126.f), 126.f));
+    uint64_t xc;
+    if constexpr (FINE) xc = pack_f32x2(clamp_nan(x0), clamp_nan(x1));
+    else xc = pack_f32x2(fminf(fmaxf(x0, -126.f), 126.f), fminf(fmaxf(x1, -126.f), 126.f));
     const uint64_t magic = pack_f32x2(12582912.f, 12582912.f);
     const uint64_t t = add_rm_f32x2(xc, magic);
     const uint64_t f = sub_f32x2(xc, sub_f32x2(t, magic));
-    uint64_t q = fma_f32x2(f, pack_f32x2(0.07711965590715408f, 0.07711965590715408f),
-                           pack_f32x2(0.2276432067155838f, 0.2276432067155838f));
-    q = fma_f32x2(q, f, pack_f32x2(0.6950892806053162f, 0.6950892806053162f));
-    q = fma_f32x2(q, f, pack_f32x2(1.f, 1.f));
+    uint64_t q;
+    if constexpr (FINE) {
+        q = fma_f32x2(f, pack_f32x2(0.013534167781472206f, 0.013534167781472206f), pack_f32x2(0.052011460065841675f, 0.052011460065841675f));
+        q = fma_f32x2(q, f, pack_f32x2(0.2414427548646927f, 0.2414427548646927f));
+        q = fma_f32x2(q, f, pack_f32x2(0.6930038332939148f, 0.6930038332939148f));
+        q = fma_f32x2(q, f, pack_f32x2(1.0000026226043701f, 1.0000026226043701f));
+    } else {
+        q = fma_f32x2(f, pack_f32x2(0.07711965590715408f, 0.07711965590715408f),
+                      pack_f32x2(0.2276432067155838f, 0.2276432067155838f));
+        q = fma_f32x2(q, f, pack_f32x2(0.6950892806053162f, 0.6950892806053162f));
+        q = fma_f32x2(q, f, pack_f32x2(1.f, 1.f));
+    }
     float q0, q1, t0, t1;
-    unpack_f32x2(q, q0, q1);
     unpack_f32x2(t, t0, t1);
+    if constexpr (FINE) {
+        const uint64_t two_j = pack_f32x2(__uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u));
+        unpack_f32x2(mul_f32x2(q, two_j), p0, p1);
+        return;
+    }
+    unpack_f32x2(q, q0, q1);
     p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
     p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
 }
@@ -195,17 +238,22 @@ struct Pass {
     int first;           // first key of the first tile
     int last;            // first key of the last tile (it ends at the image's last key if the pass does)
     int masked;          // columns of the last tile that repeat keys of the tile before, or precede key 0
-    int half;            // -1, or which half of a split item, + 2 * its slot
+    int half;            // -1, or which half of a split item, + 2 * its slot (Q4: which part, + 256 * its slot)
     int empty;
     int over;            // past the last pass of the launch
+    int parts;           // Q4: of the split item
+    int part0;           // Q4: where its first part's result goes
 };
 
 // cu, len: cu_keep and kv_len, or copies of them in shared memory.
-template <int DH>
+// Q4: the last round's items are divided into as many parts as there are slots for, of kPartTiles tiles at least.
+constexpr int kPartTiles = 6;
+template <int DH, bool Q4>
 __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu, const int32_t* len, int entry)
 {
-    constexpr int kRows = AttnCfg<DH>::kRows;
+    constexpr int kRows = AttnCfg<DH, Q4>::kRows;
     Pass r;
+    r.parts = 1;
     r.n = 0;
     r.empty = 0;
     r.over = 0;
@@ -214,14 +262,15 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     const int items = units * p.n_heads, rem = items % p.slots;
     const bool split = p.part && rem > 0 && 2 * rem <= p.slots && rem <= p.part_slots;
     const int whole = split ? items - rem : items;
-    if (entry >= whole + 2 * (items - whole)) {
+    const int max_parts = Q4 ? (split ? min(p.slots / rem, p.max_parts) : 1) : 2;
+    if (entry >= whole + max_parts * (items - whole)) {
         r.over = 1;
         return r;
     }
     int item = entry, khalf = -1, slot = 0;
     if (item >= whole) {
-        slot = (item - whole) >> 1;
-        khalf = (item - whole) & 1;
+        slot = Q4 ? (item - whole) / max_parts : (item - whole) >> 1;
+        khalf = Q4 ? (item - whole) - slot * max_parts : (item - whole) & 1;
         item = whole + slot;
     }
     const int head = item / units;
@@ -237,6 +286,22 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     r.rows_valid = min(kRows, k_b - block * kRows);
     const int n_keys = min(max(len[r.b], 0) + (p.own_keys ? k_b : 0), p.Lmax);
     const int tiles = (n_keys + BKV - 1) / BKV;
+    if constexpr (Q4) {
+        if (khalf >= 0) {
+            r.parts = max(1, min(max_parts, tiles / kPartTiles));
+            if (khalf >= r.parts) return r;
+            if (r.parts == 1) khalf = -1;
+        }
+        const int part = max(khalf, 0), t0 = tiles * part / r.parts, t1 = tiles * (part + 1) / r.parts;
+        r.n = t1 - t0;
+        r.empty = r.n == 0;
+        r.first = t0 * BKV;
+        r.last = t1 == tiles ? n_keys - BKV : (t1 - 1) * BKV;
+        r.masked = t1 == tiles ? tiles * BKV - n_keys : 0;
+        r.half = khalf < 0 ? -1 : khalf + 256 * slot;
+        r.part0 = slot * max_parts;
+        return r;
+    }
     if (khalf >= 0 && tiles < kSplitTiles) {      // too few key tiles to share: the first half takes them all
         if (khalf == 1) return r;
         khalf = -1;
@@ -251,12 +316,12 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     return r;
 }
 
-template <int DH>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int DH, bool Q4>
+__global__ void __launch_bounds__(AttnCfg<DH, Q4>::kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                  const __grid_constant__ CUtensorMap tmap_v, const AttnParams p)
 {
-    using L = AttnCfg<DH>;
+    using L = AttnCfg<DH, Q4>;
     constexpr bool kPair = L::kPair;
     constexpr int kStages = L::kStages;
     // Tensor memory: O (fp32, DH columns) at column 0, S buffer i (fp32) at 128 + 128 i; P (bf16 pairs) over the
@@ -295,15 +360,17 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         abort_flag_s = 0;
         redo_s = 0;
         for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
-        for (int i = 0; i < kStages; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&kv_full[i], Q4 ? 4 * L::kCtas : 1); mbar_init(&kv_empty[i], 1); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 4 * L::kCtas); }
         mbar_init(o_full, 1);
         mbar_init(o_empty, 4 * L::kCtas);
         for (int i = 0; i < kSlots; ++i) { mbar_init(&m_full[i], 4); mbar_init(&l_full[i], 8); }
         fence_barrier_init();
         prefetch_tmap(&tmap_q);
-        prefetch_tmap(&tmap_k);
-        prefetch_tmap(&tmap_v);
+        if constexpr (!Q4) {
+            prefetch_tmap(&tmap_k);
+            prefetch_tmap(&tmap_v);
+        }
     }
     if (warp == 1) {
         if constexpr (kPair) tmem_alloc_pair(tmem_slot, kTmemCols);
@@ -317,7 +384,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 
     // The passes of a CTA are laid out in shared memory, kTable at a time.
     Pass* table = (Pass*)(smem + L::kTabOff);
-    static_assert(kTable * sizeof(Pass) <= 64 * 44, "pass table");
+    static_assert(kTable * sizeof(Pass) <= 64 * 52, "pass table");
     const bool copy = p.B < kCuCopy;
     auto lay_out = [&](int base) {
         if (base == 0 && copy) {
@@ -325,7 +392,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             else if (threadIdx.x >= 128 && threadIdx.x < 128 + p.B) len_s[threadIdx.x - 128] = p.kv_len[threadIdx.x - 128];
         }
         __syncthreads();
-        if (threadIdx.x < kTable) table[threadIdx.x] = make_pass<DH>(p, copy ? cu_s : p.cu_keep, copy ? len_s : p.kv_len, me + (base + threadIdx.x) * stride);
+        if (threadIdx.x < kTable) table[threadIdx.x] = make_pass<DH, Q4>(p, copy ? cu_s : p.cu_keep, copy ? len_s : p.kv_len, me + (base + threadIdx.x) * stride);
         if (threadIdx.x == 0) redo_s = 0;
         __syncthreads();
     };
@@ -333,8 +400,10 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     // this launch (or ahead of the query/key transform) passed its own wait, and that GEMM has let this launch in only after
     // it. Laid out behind the wait it was 1.5 us of each launch: 20x20 scale of one image, 32 layers, 2622 -> 2590 us, 16-layer
     // 256x256 generation 8713 -> 8645, 512x512 scale 8796 -> 8744.
+    // (With a cache in 4 bits the launch ahead may be what wrote the lengths.)
+    if constexpr (Q4) pdl_wait();
     lay_out(0);
-    pdl_wait();
+    if constexpr (!Q4) pdl_wait();
 
     auto commit = [&](uint64_t* bar) {
         if constexpr (kPair) mma_commit_pair(bar, 3);
@@ -400,6 +469,23 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 if (warp == 0) {
                     if (elect_one()) {
                         bool ok = true;
+                        if constexpr (Q4) {
+                            // Q alone: the fifth warpgroup brings in keys and values
+                            for (int i = next_pass(0, only); i < kTable && ok; i = next_pass(i + 1, only))
+                                for (int pass = only ? 0 : 1; pass < 2 && ok; ++pass) {
+                                    if (qcount >= 2 && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; break; }
+                                    if (rank == 0) mbar_arrive_expect_tx(&q_full[qb], L::kCtas * L::kQBytes);
+#pragma unroll
+                                    for (int sl = 0; sl < DH / 64; ++sl) {
+                                        uint8_t* dst = smem + qb * L::kQBytes + sl * kSlabBytes;
+                                        const int row = table[i].q_begin + (int)rank * BQ;
+                                        if constexpr (kPair) tma_load_2d_pair(dst, &tmap_q, map_to_cta(smem_u32(&q_full[qb]), 0), table[i].x + sl * 64, row);
+                                        else tma_load_2d(dst, &tmap_q, &q_full[qb], table[i].x + sl * 64, row);
+                                    }
+                                    ++qcount;
+                                    if (++qb == 2) { qb = 0; qpar ^= 1u; }
+                                }
+                        }
                         // one stage: V of tile vj of pass vi (vi < 0: none) and K of the next S tile, if there is one
                         auto load_stage = [&](int vi, int vj) {
                             if (s_left == 0 && vi < 0) return;
@@ -442,8 +528,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             ++units;
                             if (++st == kStages) { st = 0; spar ^= 1u; }
                         };
-                        for (int i = 0; i < kBufs && ok; ++i) load_stage(-1, 0);
-                        for (int i = next_pass(0, only); i < kTable && ok; i = next_pass(i + 1, only)) {
+                        for (int i = 0; i < kBufs && ok && !Q4; ++i) load_stage(-1, 0);
+                        for (int i = next_pass(0, only); i < kTable && ok && !Q4; i = next_pass(i + 1, only)) {
                             const int n = table[i].n;
                             for (int pass = only ? 0 : 1; pass < 2; ++pass)        // 0: maximum pass (K only)
                                 for (int j = 0; j < n && ok; ++j) load_stage(pass ? i : -1, j);
@@ -562,6 +648,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     // nothing to attend to: the output rows are zero
                     __nv_bfloat16* dst_row = p.o + (long)(table[i].q_begin + grow) * p.C + table[i].x;
                     for (int v = 0; v < DH / 8; ++v) *(uint4*)(dst_row + v * 8) = make_uint4(0, 0, 0, 0);
+                    if (Q4 && p.lse) p.lse[(long)(table[i].x / DH) * p.M + table[i].q_begin + grow] = -INFINITY;
                 }
             do {
                 for (int i = next_pass(0, only); i < kTable; i = next_pass(i + 1, only), ++np) {
@@ -583,7 +670,13 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     // 256x256 generation took 9750 us with the trigger at the start, 9600 after the table, 9667 at
                     // the end, 9518 to 9534 here or at the first pass.
                     if (next_pass(i + 1, only) == kTable) pdl_launch_dependents();
+                    // the natural logarithm of a sum l against reference m
+                    auto put_lse = [&](float m, float l) {
+                        if (Q4 && ok && p.lse && grow < rows_valid)
+                            p.lse[(long)(table[i].x / DH) * p.M + table[i].q_begin + grow] = (fmaf(m, p.scale_log2e, kHeadroom) + log2f(l)) * 0.69314718055994531f;
+                    };
                     if (act && half < 0) {
+                        put_lse(m_ref, l_run);
                         const float inv = 1.f / l_run;
 #pragma unroll 1
                         for (int cch = 0; cch < DH / 32; ++cch) {
@@ -599,6 +692,56 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                                         pack_bf16(__uint_as_float(ov[g * 8 + 2]) * inv, __uint_as_float(ov[g * 8 + 3]) * inv),
                                         pack_bf16(__uint_as_float(ov[g * 8 + 4]) * inv, __uint_as_float(ov[g * 8 + 5]) * inv),
                                         pack_bf16(__uint_as_float(ov[g * 8 + 6]) * inv, __uint_as_float(ov[g * 8 + 7]) * inv));
+                            }
+                        }
+                    } else if (Q4 && act) {
+                        if constexpr (Q4) {
+                            // ---- a part of the keys: leave the result; who draws the last ticket adds up all parts, in their order
+                            const float c = p.scale_log2e;
+                            const int part = half & 255, tail_slot = half >> 8, parts = table[i].parts;
+                            const long stride_p = (long)(DH + 4) * L::kRows;
+                            float* all = p.part + (long)table[i].part0 * stride_p + grow;
+                            float* mine = all + part * stride_p;
+                            unsigned int* ticket = p.tickets + tail_slot * L::kCtas + rank;
+#pragma unroll 1
+                            for (int cch = 0; cch < DH / 32; ++cch) {
+                                uint32_t ov[32];
+                                tmem_ld32(o_addr + cch * 32, ov);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int g = 0; g < 32; ++g) mine[(cch * 32 + g) * L::kRows] = __uint_as_float(ov[g]);
+                            }
+                            mine[DH * L::kRows] = m_ref;
+                            mine[(DH + 1) * L::kRows] = l_run;
+                            __threadfence();
+                            asm volatile("bar.sync 1, 128;" ::: "memory");
+                            if (threadIdx.x == 128) ticket_s = atomicInc(ticket, (unsigned)parts - 1) == (unsigned)parts - 1;      // (back to zero)
+                            asm volatile("bar.sync 1, 128;" ::: "memory");
+                            if (ok && ticket_s && grow < rows_valid) {
+                                __threadfence();
+                                float top = -1e30f, l = 0.f;
+                                for (int j = 0; j < parts; ++j) top = fmaxf(top, __ldcg(all + j * stride_p + DH * L::kRows));
+                                for (int j = 0; j < parts; ++j)
+                                    l = fmaf(__ldcg(all + j * stride_p + (DH + 1) * L::kRows), ex2((__ldcg(all + j * stride_p + DH * L::kRows) - top) * c), l);
+                                put_lse(top, l);
+                                const float inv = 1.f / l;
+#pragma unroll 1
+                                for (int cch = 0; cch < DH / 32; ++cch) {
+                                    float sum[32];
+#pragma unroll
+                                    for (int g = 0; g < 32; ++g) sum[g] = 0.f;
+#pragma unroll 1
+                                    for (int j = 0; j < parts; ++j) {
+                                        const float f = ex2((__ldcg(all + j * stride_p + DH * L::kRows) - top) * c) * inv;
+#pragma unroll
+                                        for (int g = 0; g < 32; ++g) sum[g] = fmaf(__ldcg(all + j * stride_p + (cch * 32 + g) * L::kRows), f, sum[g]);
+                                    }
+                                    uint4* dst = (uint4*)(dst_row + cch * 32);
+#pragma unroll
+                                    for (int g = 0; g < 4; ++g)
+                                        dst[g] = make_uint4(pack_bf16(sum[g * 8], sum[g * 8 + 1]), pack_bf16(sum[g * 8 + 2], sum[g * 8 + 3]),
+                                                            pack_bf16(sum[g * 8 + 4], sum[g * 8 + 5]), pack_bf16(sum[g * 8 + 6], sum[g * 8 + 7]));
+                                }
                             }
                         }
                     } else if (act) {
@@ -678,7 +821,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 only = again;
             } while (true);
         }
-    } else {
+    } else if (!Q4 || warp < 16) {
         // ---- softmax ------------------------------------------------------------------------------------
         const int wg = (warp - 8) >> 2, q = warp & 3, row = q * 32 + lane;
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
@@ -783,7 +926,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                                 const uint64_t y = fma_f32x2(pack_f32x2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), c2, nm2);
                                 float p0, p1;
                                 if (e < kPolyPairs) {
-                                    exp2_poly_x2(y, p0, p1);
+                                    exp2_poly_x2<Q4>(y, p0, p1);
                                 } else {
                                     float y0, y1;
                                     unpack_f32x2(y, y0, y1);
@@ -832,6 +975,122 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             } while (true);
         }
     }
+    if constexpr (Q4) if (warp >= 16) {
+        // ---- decoding -----------------------------------------------------------------------------------
+        // Each thread brings 64 channels of one key and of one value of every stage from the cache to a ring of its own in
+        // shared memory, kRing stages ahead, and writes the decoded values to the stage as the copies of a tensor map would
+        // lie (rows of 128 bytes, the 16-byte pieces of row r exchanged by r mod 8).
+        constexpr int D = L::kRing;
+        const int dt = threadIdx.x - 512;
+        uint8_t* ring = smem + L::kRingOff + dt * 16;                      // planes of [128 threads] x 16 bytes: codes of K, of V
+        uint8_t* ring_s = smem + L::kRingOff + 128 * 64 + dt * 4;          // and [128 threads] x 4: scales of K, of V
+        const int kr = dt % L::kKRows, ks = dt / L::kKRows;               // row and slab of K
+        int st = 0, units = 0, put = 0, get = 0;
+        uint32_t spar = 0, flags = 0;                                      // what a pending unit brings: 1 K, 2 V
+        for (int base = 0; begin_round(base); base += kTable) {
+            unsigned long long only = 0;
+            do {
+                const int first_pass = only ? 0 : 1;
+                int lead = kBufs, vi = next_pass(0, only), vj = 0, vpass = first_pass;
+                int si = vi, s_n = si < kTable ? table[si].n : 0, s_left = s_n, s_passes = only ? 2 : 1;
+                auto copy64 = [&](const uint8_t* codes, const uint8_t* scales, int b, int y, int x, int plane) {
+                    const long row = (long)b * p.Lmax + max(y, 0);
+                    const uint8_t* src = codes + row * (p.C >> 1) + (x >> 1);
+                    const uint32_t dst = smem_u32(ring + put * L::kRingBytes + plane * 4096);
+                    const int live = y >= 0;                               // rows before the first read as zeros
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live * 16) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + 2048u), "l"(src + 16), "r"(live * 16) : "memory");
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(ring_s + put * L::kRingBytes + plane * 512)),
+                                 "l"(scales + row * (p.C >> 4) + (x >> 4)), "r"(live * 4) : "memory");
+                };
+                auto issue = [&]() -> bool {
+                    bool more = false;
+                    while (!more && (lead > 0 || vi < kTable)) {
+                        int has_v = 0;
+                        const int i = vi, j = vj;
+                        if (lead > 0) --lead;
+                        else {
+                            has_v = vpass;
+                            if (++vj == table[vi].n) {
+                                vj = 0;
+                                if (++vpass == 2) {
+                                    vpass = first_pass;
+                                    vi = next_pass(vi + 1, only);
+                                }
+                            }
+                        }
+                        if (has_v) {
+                            const int y = j == table[i].n - 1 ? table[i].last : table[i].first + j * BKV;
+                            copy64(p.v_codes, p.v_scales, table[i].b, y + dt, table[i].x + (int)rank * L::kVCols, 1);
+                        }
+                        const int has_k = s_left > 0;
+                        if (has_k) {
+                            const int y = s_left == 1 ? table[si].last : table[si].first + (s_n - s_left) * BKV;
+                            copy64(p.k_codes, p.k_scales, table[si].b, y + (int)rank * L::kKRows + kr, table[si].x + ks * 64, 0);
+                            if (--s_left == 0) {
+                                if (--s_passes == 0) {
+                                    si = next_pass(si + 1, only);
+                                    s_passes = only ? 2 : 1;
+                                }
+                                s_n = s_left = si < kTable ? table[si].n : 0;
+                            }
+                        }
+                        if (has_k || has_v) {
+                            flags = (flags & ~(3u << (2 * put))) | (uint32_t)(has_k + 2 * has_v) << (2 * put);
+                            if (++put == D) put = 0;
+                            more = true;
+                        }
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    return more;
+                };
+                auto decode64 = [&](int plane, uint8_t* dst_row, int r) {
+                    const uint8_t* src = ring + get * L::kRingBytes + plane * 4096;
+                    const uint32_t sc = *(const uint32_t*)(ring_s + get * L::kRingBytes + plane * 512);
+                    const uint4 a = *(const uint4*)src, b = *(const uint4*)(src + 2048);
+                    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    const c4::Scale2 s0(__byte_perm(sc, sc, 0x1010)), s1(__byte_perm(sc, sc, 0x3232));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t x[4];
+                        c4::decode8(w[i], i < 4 ? s0 : s1, x);
+                        *(uint4*)(dst_row + ((i ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+                };
+                bool ok = true;
+                int pending = 0;
+                for (int i = 0; i < D - 1; ++i) pending += issue();
+                while (pending > 0 && ok) {
+                    pending += issue();
+                    asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory");
+                    if (units >= kStages) ok = mbar_wait_warp(&kv_empty[st], spar ^ 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    uint8_t* stage = smem + L::kStageOff + st * 2 * L::kTileBytes;
+                    const uint32_t what = flags >> (2 * get) & 3u;
+                    if (what & 1u) decode64(0, stage + ks * L::kKRows * 128 + kr * 128, kr);
+                    if (what & 2u) decode64(1, stage + L::kTileBytes + dt * 128, dt);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kPair && rank != 0)
+                            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(smem_u32(&kv_full[st]), 0)) : "memory");
+                        else mbar_arrive(&kv_full[st]);
+                    }
+                    ++units;
+                    if (++st == kStages) { st = 0; spar ^= 1u; }
+                    if (++get == D) get = 0;
+                    --pending;
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                // A round ends with every use of a stage done.
+                for (int i = max(0, units - kStages); i < units && ok; ++i)
+                    ok = mbar_wait_warp(&kv_empty[i % kStages], (uint32_t)(i / kStages) & 1u, abort_flag, p.status);
+                const unsigned long long again = end_of_round();
+                if (only || !again) break;
+                only = again;
+            } while (true);
+        }
+    }
     // (the last end_of_round saw everybody's work done: nobody signals this CTA any more)
     tc_fence_before();
     __syncwarp();
@@ -846,7 +1105,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 template <int DH>
 nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
 {
-    using L = AttnCfg<DH>;
+    using L = AttnCfg<DH, false>;
     CUtensorMap tq, tk, tv;
     const uint64_t dq[2] = {(uint64_t)a.C, (uint64_t)a.M}, sq[1] = {(uint64_t)a.C * 2};
     const uint64_t dk[3] = {(uint64_t)a.C, (uint64_t)a.Lmax, (uint64_t)a.B};
@@ -855,11 +1114,12 @@ nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
         !make_tmap_bf16(ctx, &tv, a.v_cache, 3, dk, sk, BKV))
         return nova_fail(ctx, NOVA_ERR_CUDA, "attention: cuTensorMapEncodeTiled failed");
     if (!ctx->attr_attn) {   // both head sizes once per context
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64>::kTotal));
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, false>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, false>::kTotal));
         ctx->attr_attn = true;
     }
     AttnParams p;
+    memset(&p, 0, sizeof(p));
     p.cu_keep = a.cu_keep; p.kv_len = a.kv_len; p.o = a.o; p.B = a.B; p.C = a.C; p.Lmax = a.Lmax;
     p.scale_log2e = (float)((1.0 / sqrt((double)DH)) * 1.4426950408889634);
     p.status = ctx->dev_status;
@@ -878,12 +1138,61 @@ nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
     const int ctas = (int)min((long)p.slots, (can_split ? 2 : 1) * items) * L::kCtas;
     {
         nova_launch_scope scope(ctx, NOVA_K_ATTENTION, st);
-        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH>, dim3(ctas), dim3(kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
+        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, false>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
+    }
+    return NOVA_OK;
+}
+
+template <int DH>
+nova_status launch4(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
+{
+    using L = AttnCfg<DH, true>;
+    const nova_cache4& c = *a.cache;
+    CUtensorMap tq;
+    const uint64_t dq[2] = {(uint64_t)c.C, (uint64_t)a.M}, sq[1] = {(uint64_t)a.ldq * 2};
+    if (!make_tmap_bf16(ctx, &tq, a.q, 2, dq, sq, BQ)) return nova_fail(ctx, NOVA_ERR_CUDA, "cache4 attention: cuTensorMapEncodeTiled failed");
+    if (!ctx->attr_attn4) {   // both head sizes once per context
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, true>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, true>::kTotal));
+        ctx->attr_attn4 = true;
+    }
+    AttnParams p;
+    memset(&p, 0, sizeof(p));
+    p.cu_keep = a.cu; p.kv_len = c.kv_len; p.o = a.o; p.B = c.B; p.C = c.C; p.Lmax = c.Lmax;
+    p.scale_log2e = (float)((1.0 / sqrt((double)DH)) * 1.4426950408889634);
+    p.status = ctx->dev_status;
+    p.n_heads = c.n_heads; p.slots = ctx->num_sms / L::kCtas;
+    p.own_keys = a.own_rows;
+    p.k_codes = (const uint8_t*)c.k_codes; p.v_codes = (const uint8_t*)c.v_codes;
+    p.k_scales = (const uint8_t*)c.k_scales; p.v_scales = (const uint8_t*)c.v_scales;
+    p.lse = a.lse; p.M = a.M;
+    // the last round's items may be shared: at most slots / 2 items, in parts of which all together fill the slots
+    const bool can_split = (c.Lmax + BKV - 1) / BKV >= 2 * kPartTiles;
+    p.part = can_split ? (float*)a.scratch : nullptr;
+    p.part_slots = NOVA_ATTN_TICKETS / L::kCtas;
+    p.max_parts = 255;
+    p.tickets = ctx->dev_status + NOVA_ATTN_TICKET_WORD0;
+    const long items = (((long)a.M + (long)c.B * (L::kRows - 1)) / L::kRows) * c.n_heads;
+    const long most = can_split ? items * ((c.Lmax + BKV - 1) / BKV / kPartTiles) : items;
+    const int ctas = (int)min((long)p.slots, most) * L::kCtas;
+    {
+        nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
+        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, true>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tq, tq, p));
     }
     return NOVA_OK;
 }
 
 }  // namespace
+
+size_t nova_cache4_tiles_scratch(int num_sms, int dh)
+{
+    // (parts) x (rows) x (columns): parts of all split items together are no more than the CTAs (pairs) that run at once
+    return (size_t)num_sms * BQ * (dh + 4) * sizeof(float);
+}
+nova_status nova_launch_cache4_tiles(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
+{
+    return a.cache->C / a.cache->n_heads == 64 ? launch4<64>(ctx, a, st) : launch4<128>(ctx, a, st);
+}
 
 nova_status nova_launch_attention(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
 {

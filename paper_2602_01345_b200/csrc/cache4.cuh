@@ -91,6 +91,9 @@ struct nova_cache4_attn_args {
 };
 size_t nova_cache4_attention_scratch(int num_sms, int dh, int M);
 nova_status nova_launch_cache4_attention(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st);
+// The same on the tensor cores' 128-row tiles (attention.cu).
+size_t nova_cache4_tiles_scratch(int num_sms, int dh);
+nova_status nova_launch_cache4_tiles(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st);
 size_t nova_cache4_weights_scratch(int num_sms);
 nova_status nova_launch_cache4_weights(nova_ctx* ctx, const nova_cache4* c, const __nv_bfloat16* q, int64_t ldq, const float* lse, const int32_t* cu,
                                        int M, const float* in, float* out, bool own_rows, void* scratch, size_t scratch_bytes, cudaStream_t st);

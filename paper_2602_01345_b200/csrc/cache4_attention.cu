@@ -22,6 +22,7 @@ namespace {
 using namespace c4;
 
 constexpr int kFewRows = 16;           // query rows of a unit
+constexpr long kFewPerImage = 24;      // rows per image, on average, up to which the launch takes this kernel
 constexpr int kWarpKeys = 32;          // keys of a warp's tile
 constexpr float kRescale = 8.f;        // the maximum follows when it is exceeded by more than this (log2)
 
@@ -67,7 +68,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // Copies to shared memory of which `live` = 0 writes zeros and reads nothing.
@@ -83,31 +84,6 @@ __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, bo
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint16_t lds16(uint32_t a)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-    return v;
-}
-
 // A place in the launch's tiles: tile t of unit (b, head, block), of which the image has `units`, with T tiles each.
 template <int DH>
 struct FewWalk {
@@ -198,7 +174,7 @@ cache4_few_kernel(const FewParams p)
     const long first = W * blockIdx.x / G, end = W * (blockIdx.x + 1) / G;
     auto cta_of = [&](long tile) { return (int)(((tile + 1) * G - 1) / W); };     // the CTA whose range holds this tile
 
-    const uint32_t ring = tc::smem_u32(smem + L::kRingOff) + (uint32_t)(warp * L::kDepth * L::kStageBytes);
+    uint8_t* ring = smem + L::kRingOff + warp * L::kDepth * L::kStageBytes;
     constexpr uint32_t kVOff = kWarpKeys * L::kRowBytes, kKsOff = 2 * kVOff, kVsOff = kKsOff + kWarpKeys * L::kScaleBytes;
     // Row of a V stage in which key n of the warp's tile lies, and the exchange of its 16-byte pieces: such that the 32
     // threads' reads of four rows touch every bank once.
@@ -213,7 +189,7 @@ cache4_few_kernel(const FewParams p)
         if (issued < end) {
             const int key0 = pf.t * L::kTile + warp * kWarpKeys;
             if (pf.len > key0) {
-                const uint32_t s = ring + (uint32_t)(slot * L::kStageBytes);
+                const uint32_t s = tc::smem_u32(ring + slot * L::kStageBytes);
                 const int head = pf.unit % p.n_heads;
                 const long base = (long)pf.b * p.Lmax;
                 constexpr int kPieces = L::kRowBytes / 16;
@@ -276,20 +252,20 @@ cache4_few_kernel(const FewParams p)
             __syncwarp();
             const int key0 = (int)(tile - row0) * L::kTile + warp * kWarpKeys;
             if (key0 < len) {
-                const uint32_t s_at = ring + (uint32_t)(slot * L::kStageBytes);
+                const uint8_t* s_at = ring + slot * L::kStageBytes;
                 float s[4][4];
 #pragma unroll
                 for (int nb = 0; nb < 4; ++nb) {
                     s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
                     const int n = nb * 8 + g;
                     // dh 128: this thread's 32 channels are one group; dh 64: its 16 are half of one
-                    const Scale2 sc(both(lds16(s_at + kKsOff + (uint32_t)(n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2))));
+                    const Scale2 sc(both(*(const uint16_t*)(s_at + kKsOff + n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2)));
                     uint32_t w[4];
                     if constexpr (DH == 128) {
-                        const uint4 v = lds128(s_at + (uint32_t)(n * L::kRowBytes + t * 16));
+                        const uint4 v = *(const uint4*)(s_at + n * L::kRowBytes + t * 16);
                         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
                     } else {
-                        const uint2 v = lds64(s_at + (uint32_t)(n * L::kRowBytes + t * 8));
+                        const uint2 v = *(const uint2*)(s_at + n * L::kRowBytes + t * 8);
                         w[0] = v.x; w[1] = v.y; w[2] = w[3] = 0;
                     }
 #pragma unroll
@@ -357,14 +333,14 @@ cache4_few_kernel(const FewParams p)
                         for (int e = 0; e < 2; ++e) {
                             const int row = 16 * kb + 8 * h + 4 * e + t;         // v_row of key 16 kb + 8 h + 2 t + e
                             if constexpr (DH == 128) {
-                                const uint2 v = lds64(s_at + kVOff + (uint32_t)(row * L::kRowBytes + (((g >> 1) ^ v_swap(row)) * 16 + (g & 1) * 8)));
+                                const uint2 v = *(const uint2*)(s_at + kVOff + row * L::kRowBytes + ((g >> 1) ^ v_swap(row)) * 16 + (g & 1) * 8);
                                 wv[e][0] = v.x; wv[e][1] = v.y;
                             } else {
-                                wv[e][0] = lds32(s_at + kVOff + (uint32_t)(row * L::kRowBytes + g * 4));
+                                wv[e][0] = *(const uint32_t*)(s_at + kVOff + row * L::kRowBytes + g * 4);
                                 wv[e][1] = 0;
                             }
                             const int n = 16 * kb + 8 * h + 2 * t + e;
-                            sv[e] = lds16(s_at + kVsOff + (uint32_t)(n * L::kScaleBytes + (DH == 128 ? g >> 1 : g >> 2) * 2));
+                            sv[e] = *(const uint16_t*)(s_at + kVsOff + n * L::kScaleBytes + (DH == 128 ? g >> 1 : g >> 2) * 2);
                         }
 #pragma unroll
                         for (int w = 0; w < kBlocks / 8; ++w) {
@@ -547,7 +523,7 @@ nova_status launch_few(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream
 size_t nova_cache4_attention_scratch(int num_sms, int dh, int M)
 {
     if (M <= 0) return 0;
-    return (size_t)num_sms * 2 * kFewRows * (dh + 2) * sizeof(float);
+    return max((size_t)num_sms * 2 * kFewRows * (dh + 2) * sizeof(float), nova_cache4_tiles_scratch(num_sms, dh));
 }
 
 nova_status nova_launch_cache4_attention(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
@@ -556,6 +532,7 @@ nova_status nova_launch_cache4_attention(nova_ctx* ctx, const nova_cache4_attn_a
     const int dh = a.cache->C / a.cache->n_heads;
     if (!a.scratch || a.scratch_bytes < nova_cache4_attention_scratch(ctx->num_sms, dh, a.M))
         return nova_fail(ctx, NOVA_ERR_WORKSPACE, "nova_cache4_attention: workspace missing or too small");
+    if ((long)a.M > kFewPerImage * (long)a.cache->B) return nova_launch_cache4_tiles(ctx, a, st);
     return dh == 64 ? launch_few<64>(ctx, a, st) : launch_few<128>(ctx, a, st);
 }
 
