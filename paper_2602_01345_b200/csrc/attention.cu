@@ -49,7 +49,7 @@ constexpr int BQ = 128;        // query rows per CTA
 constexpr int BKV = 128;       // keys per tile
 constexpr int kBufs = 3;       // S buffers in tensor memory
 constexpr int kThreads512 = 512;  // warpgroups: producer + issuer (+2 idle warps), epilogue, softmax 0, softmax 1
-constexpr int kThreads4 = 640; // and one that decodes keys and values, with a cache in 4 bits
+constexpr int kThreads4 = 768; // and, with a cache in 4 bits, one that decodes keys and one that decodes values
 constexpr int kSlabBytes = 128 * 128;   // [128 rows][64 bf16]
 // The probability of a score equal to the reference is 2^-kHeadroom. A row's sum of probabilities over one key tile at
 // or above kHugeSum (or NaN) means a score about 2^(80 + kHeadroom) above the reference. That is far below
@@ -74,16 +74,17 @@ struct AttnCfg {
     static constexpr int kTileBytes = kKRows * DH * 2;          // K and V alike (BKV * kVCols * 2)
     static constexpr int kStages = Q4 ? 3 : kPair ? 4 : 5;      // stage: K of a tile and V of the tile kBufs before it
     static constexpr int kStageOff = 2 * kQBytes;
-    static constexpr int kLOff = kStageOff + kStages * 2 * kTileBytes;  // [kSlots][2][128] row sums of the two warpgroups
+    // Q4: a ring of packed tiles: codes of K [kKRows][DH / 2 bytes], of V [128][32 bytes] (as tensor maps exchange their 16-byte
+    // pieces), scales of K and V [128 threads] x 4 bytes
+    static constexpr int kRing = Q4 ? 5 : 0;
+    static constexpr int kRingBytes = 4096 + 4096 + 512 + 512;
+    static constexpr int kRingOff = kStageOff + kStages * 2 * kTileBytes;
+    static constexpr int kLOff = kRingOff + kRing * kRingBytes;         // [kSlots][2][128] row sums of the two warpgroups
     static constexpr int kMOff = kLOff + kSlots * 2 * BQ * 4;           // [kSlots][128] reference maxima
     static constexpr int kAOff = kMOff + kSlots * BQ * 4;               // [2][128] maxima of a maximum pass
     static constexpr int kTabOff = kAOff + 2 * BQ * 4;                  // [kTable] passes
     static constexpr int kBarOff = kTabOff + 64 * 52;
-    // Q4: [kRing][2][128 threads] pieces of 32 bytes of codes (as two planes of 16), and their scales
-    static constexpr int kRing = 5;
-    static constexpr int kRingBytes = 128 * 2 * (32 + 4);
-    static constexpr int kRingOff = kBarOff + 512;
-    static constexpr int kTotal = kBarOff + 512 + 1024 + (Q4 ? kRing * kRingBytes : 0);
+    static constexpr int kTotal = kBarOff + 512 + 1024;
     static_assert(kTotal <= 227 * 1024, "shared memory");
     static_assert(kKRows * (DH / 64) == 128 && 128 * (kVCols / 64) == 128, "a decoding thread has 64 channels of a key and of a value");
     static_assert(kVCols == 64, "a V stage is one 128-byte-wide slab");
@@ -316,10 +317,47 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     return r;
 }
 
+// Q4: the parts of split items become their output rows, added in the order of the parts: a row and eight columns per thread. (By the
+// epilogue's warpgroup alone, a row per thread, it took 30 us.)
+template <int DH>
+__device__ __noinline__ void merge_parts(const AttnParams& p, const Pass* table, unsigned long long passes, int rank)
+{
+    constexpr int kRows = AttnCfg<DH, true>::kRows;
+    constexpr long kPart = (long)(DH + 4) * kRows;
+    const float c = p.scale_log2e;
+    __threadfence();
+    for (; passes; passes &= passes - 1) {
+        const Pass& t = table[__ffsll((long long)passes) - 1];
+        const int parts = t.parts, rows = min(BQ, t.rows_valid - rank * BQ), head = t.x / DH;
+        for (int at = threadIdx.x; at < BQ * (DH / 8); at += blockDim.x) {
+            const int row = at % BQ, col = at / BQ * 8;
+            if (row >= rows) continue;
+            const float* all = p.part + (long)t.part0 * kPart + rank * BQ + row;
+            float top = -1e30f, l = 0.f, sum[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) sum[g] = 0.f;
+            for (int j = 0; j < parts; ++j) top = fmaxf(top, __ldcg(all + j * kPart + DH * kRows));
+#pragma unroll 4
+            for (int j = 0; j < parts; ++j) {
+                const float* part = all + j * kPart;
+                const float f = ex2((__ldcg(part + DH * kRows) - top) * c);
+                l = fmaf(__ldcg(part + (DH + 1) * kRows), f, l);
+#pragma unroll
+                for (int g = 0; g < 8; ++g) sum[g] = fmaf(__ldcg(part + (col + g) * kRows), f, sum[g]);
+            }
+            const float inv = 1.f / l;
+            const long r = t.q_begin + rank * BQ + row;
+            *(uint4*)(p.o + r * p.C + t.x + col) = make_uint4(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv),
+                                                              pack_bf16(sum[4] * inv, sum[5] * inv), pack_bf16(sum[6] * inv, sum[7] * inv));
+            if (p.lse && col == 0) p.lse[(long)head * p.M + r] = (fmaf(top, c, kHeadroom) + log2f(l)) * 0.69314718055994531f;
+        }
+    }
+}
+
 template <int DH, bool Q4>
 __global__ void __launch_bounds__(AttnCfg<DH, Q4>::kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
-                 const __grid_constant__ CUtensorMap tmap_v, const AttnParams p)
+                 const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AttnParams p)
 {
     using L = AttnCfg<DH, Q4>;
     constexpr bool kPair = L::kPair;
@@ -343,9 +381,13 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     uint64_t* o_empty = o_full + 1;                   // 1 *, one arrival per epilogue warp
     uint64_t* m_full = o_empty + 1;                   // kSlots, one arrival per warp of the first tile's warpgroup
     uint64_t* l_full = m_full + kSlots;               // kSlots, one arrival per softmax warp
-    uint32_t* tmem_slot = (uint32_t*)(l_full + kSlots);
+    uint64_t* r_full = l_full + kSlots;               // Q4: kRing, one arrival per loading thread and one more
+    uint64_t* r_empty = r_full + L::kRing;            // Q4: kRing, one arrival per warp of the tile's decoding warpgroup
+    uint32_t* tmem_slot = (uint32_t*)(r_empty + L::kRing);
+    __shared__ int ring_s[Q4 ? L::kRing : 1];         // Q4: what a ring slot brings: 1 keys, 2 values; at the end of a round -1 - stages so far
     __shared__ int abort_flag_s;
     __shared__ int ticket_s;
+    __shared__ unsigned long long merge_s;            // Q4: passes of the round whose item this CTA merges
     __shared__ unsigned long long redo_s;             // passes of the round in which a row sum was huge in this CTA
     __shared__ unsigned long long redo_peer_s;        // the same of the pair's other CTA, written by it
     constexpr int kCuCopy = 64;
@@ -358,6 +400,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 
     if (threadIdx.x == 0) {
         abort_flag_s = 0;
+        merge_s = 0;
         redo_s = 0;
         for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
         for (int i = 0; i < kStages; ++i) { mbar_init(&kv_full[i], Q4 ? 4 * L::kCtas : 1); mbar_init(&kv_empty[i], 1); }
@@ -365,12 +408,11 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         mbar_init(o_full, 1);
         mbar_init(o_empty, 4 * L::kCtas);
         for (int i = 0; i < kSlots; ++i) { mbar_init(&m_full[i], 4); mbar_init(&l_full[i], 8); }
+        for (int i = 0; Q4 && i < L::kRing; ++i) { mbar_init(&r_full[i], 64 + 1); mbar_init(&r_empty[i], 4); }
         fence_barrier_init();
         prefetch_tmap(&tmap_q);
-        if constexpr (!Q4) {
-            prefetch_tmap(&tmap_k);
-            prefetch_tmap(&tmap_v);
-        }
+        prefetch_tmap(&tmap_k);
+        prefetch_tmap(&tmap_v);
     }
     if (warp == 1) {
         if constexpr (kPair) tmem_alloc_pair(tmem_slot, kTmemCols);
@@ -426,6 +468,14 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     auto end_of_round = [&]() -> unsigned long long {
         __syncwarp();
         __syncthreads();
+        if constexpr (Q4) {
+            const unsigned long long merges = *(volatile unsigned long long*)&merge_s;
+            if (merges) {
+                if (!*abort_flag) merge_parts<DH>(p, table, merges, (int)rank);
+                __syncthreads();
+                if (threadIdx.x == 0) merge_s = 0;
+            }
+        }
         unsigned long long mask = *(volatile unsigned long long*)&redo_s;
         if constexpr (kPair) {
             if (threadIdx.x == 0)
@@ -446,9 +496,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     };
 
     if (warp < 4) {
-        int st = 0, qb = 0;                            // ring positions
-        uint32_t spar = 0, qpar = 0;                   // and their phase parities
-        int units = 0, qcount = 0;                     // loaded so far (producer)
+        int st = 0, qb = 0, rs = 0;                    // ring positions
+        uint32_t spar = 0, qpar = 0, rpar = 0;         // and their phase parities
+        int units = 0, qcount = 0, stages = 0;         // loaded so far (producer)
         int sbuf = 0, pbuf = 0;                        // S buffer of the next S, of the next P (issuer)
         uint32_t ppar = 0, opar = 1;
         bool o_used = false;
@@ -470,7 +520,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     if (elect_one()) {
                         bool ok = true;
                         if constexpr (Q4) {
-                            // Q alone: the fifth warpgroup brings in keys and values
+                            // Q alone: the last two warpgroups bring in keys and values
                             for (int i = next_pass(0, only); i < kTable && ok; i = next_pass(i + 1, only))
                                 for (int pass = only ? 0 : 1; pass < 2 && ok; ++pass) {
                                     if (qcount >= 2 && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; break; }
@@ -628,6 +678,75 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         }
                     }
                 }
+                if constexpr (Q4) if (warp >= 2) {
+                    // Warps 2 and 3 bring the packed tiles into the ring, in the order in which the stages want them: codes by tensor
+                    // maps, scales, whose rows per head are too short for those, by copies of 4 bytes. (Copies made by the decoding
+                    // threads themselves hold up their fences and arrivals; with the codes copied here in pieces of 16 bytes the
+                    // two warps needed 0.75 us per tile.)
+                    const int lt = threadIdx.x - 64;
+                    int lead = kBufs, vi = next_pass(0, only), vj = 0, vpass = only ? 0 : 1, ends = 0;
+                    bool ok = true;
+                    const int scale_row = p.C >> 4;
+                    auto copy_scales = [&](uint32_t dst, const uint8_t* src, bool live) {
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
+                    };
+                    while (ends < 2) {
+                        bool has_v = false;
+                        const int i = vi, j = vj;
+                        const bool over = lead == 0 && vi >= kTable;
+                        if (lead > 0) --lead;
+                        else if (!over) {
+                            has_v = vpass == 1;
+                            if (++vj == table[vi].n) {
+                                vj = 0;
+                                if (++vpass == 2) {
+                                    vpass = only ? 0 : 1;
+                                    vi = next_pass(vi + 1, only);
+                                }
+                            }
+                        }
+                        const bool has_k = s_left > 0;
+                        if (!over && !has_k && !has_v) continue;
+                        if (units >= L::kRing) ok = mbar_wait_warp(&r_empty[rs], rpar ^ 1u, abort_flag, p.status);
+                        if (!ok) break;
+                        uint8_t* const to = smem + L::kRingOff + rs * L::kRingBytes;
+                        const int si_now = si, yk = !has_k ? 0 : (s_left == 1 ? table[si].last : table[si].first + (s_n - s_left) * BKV) + (int)rank * L::kKRows;
+                        const int yv = !has_v ? 0 : j == table[i].n - 1 ? table[i].last : table[i].first + j * BKV;
+                        if (has_k) s_step();
+                        if (warp == 2 && elect_one()) {
+                            ring_s[rs] = over ? -1 - stages : (has_k ? 1 : 0) | (has_v ? 2 : 0);
+                            mbar_arrive_expect_tx(&r_full[rs], (has_k ? 4096 : 0) + (has_v ? 4096 : 0));
+                            // (rows before the first read as zeros)
+                            if (has_k) tma_load_3d(to, &tmap_k, &r_full[rs], table[si_now].x >> 1, yk, table[si_now].b);
+                            if (has_v) tma_load_3d(to + 4096, &tmap_v, &r_full[rs], (table[i].x + (int)rank * L::kVCols) >> 1, yv, table[i].b);
+                        }
+                        __syncwarp();
+                        if (has_k) {
+                            const uint8_t* scales = p.k_scales + (long)table[si_now].b * p.Lmax * scale_row + (table[si_now].x >> 4);
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const int at = c * 64 + lt, r = at / (DH / 64), sl = at % (DH / 64);
+                                copy_scales(smem_u32(to) + (uint32_t)(8192 + (sl * L::kKRows + r) * 4), scales + (long)max(yk + r, 0) * scale_row + sl * 4, yk + r >= 0);
+                            }
+                        }
+                        if (has_v) {
+                            const uint8_t* scales = p.v_scales + (long)table[i].b * p.Lmax * scale_row + ((table[i].x + (int)rank * L::kVCols) >> 4);
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const int r = c * 64 + lt;
+                                copy_scales(smem_u32(to) + (uint32_t)(8704 + r * 4), scales + (long)max(yv + r, 0) * scale_row, yv + r >= 0);
+                            }
+                        }
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[rs])) : "memory");
+                        ++units;
+                        if (over) ++ends;              // (one for each of the two warpgroups that take turns)
+                        else ++stages;
+                        if (++rs == L::kRing) { rs = 0; rpar ^= 1u; }
+                    }
+                    if (!ok || *abort_flag)            // what is in flight gets some time to finish before memory is released
+                        for (int i = max(0, units - L::kRing); i < units; ++i) mbar_drain(&r_full[i % L::kRing], (uint32_t)(i / L::kRing) & 1u);
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                }
                 const unsigned long long again = end_of_round();
                 if (only || !again) break;
                 only = again;
@@ -696,8 +815,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         }
                     } else if (Q4 && act) {
                         if constexpr (Q4) {
-                            // ---- a part of the keys: leave the result; who draws the last ticket adds up all parts, in their order
-                            const float c = p.scale_log2e;
+                            // ---- a part of the keys: leave the result; the CTA that draws the last ticket merges all parts at the end of the
+                            // round, with all its warps
                             const int part = half & 255, tail_slot = half >> 8, parts = table[i].parts;
                             const long stride_p = (long)(DH + 4) * L::kRows;
                             float* all = p.part + (long)table[i].part0 * stride_p + grow;
@@ -715,34 +834,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             mine[(DH + 1) * L::kRows] = l_run;
                             __threadfence();
                             asm volatile("bar.sync 1, 128;" ::: "memory");
-                            if (threadIdx.x == 128) ticket_s = atomicInc(ticket, (unsigned)parts - 1) == (unsigned)parts - 1;      // (back to zero)
-                            asm volatile("bar.sync 1, 128;" ::: "memory");
-                            if (ok && ticket_s && grow < rows_valid) {
-                                __threadfence();
-                                float top = -1e30f, l = 0.f;
-                                for (int j = 0; j < parts; ++j) top = fmaxf(top, __ldcg(all + j * stride_p + DH * L::kRows));
-                                for (int j = 0; j < parts; ++j)
-                                    l = fmaf(__ldcg(all + j * stride_p + (DH + 1) * L::kRows), ex2((__ldcg(all + j * stride_p + DH * L::kRows) - top) * c), l);
-                                put_lse(top, l);
-                                const float inv = 1.f / l;
-#pragma unroll 1
-                                for (int cch = 0; cch < DH / 32; ++cch) {
-                                    float sum[32];
-#pragma unroll
-                                    for (int g = 0; g < 32; ++g) sum[g] = 0.f;
-#pragma unroll 1
-                                    for (int j = 0; j < parts; ++j) {
-                                        const float f = ex2((__ldcg(all + j * stride_p + DH * L::kRows) - top) * c) * inv;
-#pragma unroll
-                                        for (int g = 0; g < 32; ++g) sum[g] = fmaf(__ldcg(all + j * stride_p + (cch * 32 + g) * L::kRows), f, sum[g]);
-                                    }
-                                    uint4* dst = (uint4*)(dst_row + cch * 32);
-#pragma unroll
-                                    for (int g = 0; g < 4; ++g)
-                                        dst[g] = make_uint4(pack_bf16(sum[g * 8], sum[g * 8 + 1]), pack_bf16(sum[g * 8 + 2], sum[g * 8 + 3]),
-                                                            pack_bf16(sum[g * 8 + 4], sum[g * 8 + 5]), pack_bf16(sum[g * 8 + 6], sum[g * 8 + 7]));
-                                }
-                            }
+                            if (threadIdx.x == 128 && atomicInc(ticket, (unsigned)parts - 1) == (unsigned)parts - 1)      // (back to zero)
+                                atomicOr(&merge_s, 1ull << i);
                         }
                     } else if (act) {
                         const int khalf = half & 1, tail_slot = half >> 1;
@@ -844,6 +937,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             do {
             for (int i = next_pass(0, only); i < kTable; i = next_pass(i + 1, only)) {
             const int n = table[i].n, masked = table[i].masked;
+            // A warp without rows of this item leaves its P as it is: rows of the product that nobody reads. (Not with bf16 caches, whose
+            // rounding must stay what it is where a later image's rows are in the tile.)
+            const bool idle = Q4 && (int)rank * BQ + q * 32 >= table[i].rows_valid;
             float m_true = -1e30f;             // the row's maximum over all keys, from a maximum pass
             for (int pass = only ? 0 : 1; pass < 2; ++pass) {
                 const int slot = np % kSlots;
@@ -862,6 +958,17 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     // The row is taken 32 scores at a time, in loops that are not unrolled: the code of a whole
                     // row is 16 KB, and fetching it costs a launch's first tile 6 us. The latency of the
                     // tensor-memory reads hides behind the other warpgroup.
+                    if (idle) {
+                        if (pass == 1 && j == 0) {
+                            m_s[slot * BQ] = 0.f;
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&m_full[slot]);
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) arrive_leader(done);
+                        continue;
+                    }
                     const int skip = j == n - 1 ? masked : 0;       // columns that do not count
                     auto load = [&](int ch, uint32_t (&sv)[32]) {
                         tmem_ld32(s_addr + ch * 32, sv);
@@ -977,113 +1084,71 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     }
     if constexpr (Q4) if (warp >= 16) {
         // ---- decoding -----------------------------------------------------------------------------------
-        // Each thread brings 64 channels of one key and of one value of every stage from the cache to a ring of its own in
-        // shared memory, kRing stages ahead, and writes the decoded values to the stage as the copies of a tensor map would
-        // lie (rows of 128 bytes, the 16-byte pieces of row r exchanged by r mod 8).
-        constexpr int D = L::kRing;
-        const int dt = threadIdx.x - 512;
-        uint8_t* ring = smem + L::kRingOff + dt * 16;                      // planes of [128 threads] x 16 bytes: codes of K, of V
-        uint8_t* ring_s = smem + L::kRingOff + 128 * 64 + dt * 4;          // and [128 threads] x 4: scales of K, of V
-        const int kr = dt % L::kKRows, ks = dt / L::kKRows;               // row and slab of K
-        int st = 0, units = 0, put = 0, get = 0;
-        uint32_t spar = 0, flags = 0;                                      // what a pending unit brings: 1 K, 2 V
+        // Two warpgroups that take the stages in turn: each thread 64 channels of a key and 64 of a value, from the ring to the stage,
+        // where they lie as the copies of a tensor map would (rows of 128 bytes, the 16-byte pieces of row r exchanged by r mod 8).
+        // (3277 rows x 29414 keys, us: one warpgroup for all 1184; one for keys and one for values, whose waits and hand-overs are then
+        // paid by each stage, 904.)
+        const int dt = threadIdx.x & 127;
+        const int k_row = dt % L::kKRows, k_slab = dt / L::kKRows;
+        uint8_t* const k_to = smem + L::kStageOff + k_slab * L::kKRows * 128 + k_row * 128;
+        uint8_t* const v_to = smem + L::kStageOff + L::kTileBytes + dt * 128;
+        // the exchange of 16-byte pieces in the ring: of rows of 64 bytes by (row / 2) mod 4, of 32 bytes by (row / 4) mod 2
+        const int k_at = DH == 128 ? k_row * 64 : k_row * 32, k_swap = DH == 128 ? k_row >> 1 & 3 : k_row >> 2 & 1;
+        const int v_at = 4096 + dt * 32, v_swap = dt >> 2 & 1;
+        int u = (warp - 16) >> 2, ended = 0;               // ring entry, ends of rounds among those before it
         for (int base = 0; begin_round(base); base += kTable) {
             unsigned long long only = 0;
             do {
-                const int first_pass = only ? 0 : 1;
-                int lead = kBufs, vi = next_pass(0, only), vj = 0, vpass = first_pass;
-                int si = vi, s_n = si < kTable ? table[si].n : 0, s_left = s_n, s_passes = only ? 2 : 1;
-                auto copy64 = [&](const uint8_t* codes, const uint8_t* scales, int b, int y, int x, int plane) {
-                    const long row = (long)b * p.Lmax + max(y, 0);
-                    const uint8_t* src = codes + row * (p.C >> 1) + (x >> 1);
-                    const uint32_t dst = smem_u32(ring + put * L::kRingBytes + plane * 4096);
-                    const int live = y >= 0;                               // rows before the first read as zeros
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live * 16) : "memory");
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + 2048u), "l"(src + 16), "r"(live * 16) : "memory");
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(ring_s + put * L::kRingBytes + plane * 512)),
-                                 "l"(scales + row * (p.C >> 4) + (x >> 4)), "r"(live * 4) : "memory");
-                };
-                auto issue = [&]() -> bool {
-                    bool more = false;
-                    while (!more && (lead > 0 || vi < kTable)) {
-                        int has_v = 0;
-                        const int i = vi, j = vj;
-                        if (lead > 0) --lead;
-                        else {
-                            has_v = vpass;
-                            if (++vj == table[vi].n) {
-                                vj = 0;
-                                if (++vpass == 2) {
-                                    vpass = first_pass;
-                                    vi = next_pass(vi + 1, only);
-                                }
-                            }
-                        }
-                        if (has_v) {
-                            const int y = j == table[i].n - 1 ? table[i].last : table[i].first + j * BKV;
-                            copy64(p.v_codes, p.v_scales, table[i].b, y + dt, table[i].x + (int)rank * L::kVCols, 1);
-                        }
-                        const int has_k = s_left > 0;
-                        if (has_k) {
-                            const int y = s_left == 1 ? table[si].last : table[si].first + (s_n - s_left) * BKV;
-                            copy64(p.k_codes, p.k_scales, table[si].b, y + (int)rank * L::kKRows + kr, table[si].x + ks * 64, 0);
-                            if (--s_left == 0) {
-                                if (--s_passes == 0) {
-                                    si = next_pass(si + 1, only);
-                                    s_passes = only ? 2 : 1;
-                                }
-                                s_n = s_left = si < kTable ? table[si].n : 0;
-                            }
-                        }
-                        if (has_k || has_v) {
-                            flags = (flags & ~(3u << (2 * put))) | (uint32_t)(has_k + 2 * has_v) << (2 * put);
-                            if (++put == D) put = 0;
-                            more = true;
-                        }
-                    }
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    return more;
-                };
-                auto decode64 = [&](int plane, uint8_t* dst_row, int r) {
-                    const uint8_t* src = ring + get * L::kRingBytes + plane * 4096;
-                    const uint32_t sc = *(const uint32_t*)(ring_s + get * L::kRingBytes + plane * 512);
-                    const uint4 a = *(const uint4*)src, b = *(const uint4*)(src + 2048);
-                    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                    const c4::Scale2 s0(__byte_perm(sc, sc, 0x1010)), s1(__byte_perm(sc, sc, 0x3232));
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t x[4];
-                        c4::decode8(w[i], i < 4 ? s0 : s1, x);
-                        *(uint4*)(dst_row + ((i ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-                    }
-                };
                 bool ok = true;
-                int pending = 0;
-                for (int i = 0; i < D - 1; ++i) pending += issue();
-                while (pending > 0 && ok) {
-                    pending += issue();
-                    asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory");
-                    if (units >= kStages) ok = mbar_wait_warp(&kv_empty[st], spar ^ 1u, abort_flag, p.status);
+                int done = 0;
+                for (;; u += 2) {
+                    const int rs = u % L::kRing;
+                    ok = mbar_wait_warp(&r_full[rs], (uint32_t)(u / L::kRing) & 1u, abort_flag, p.status);
                     if (!ok) break;
-                    uint8_t* stage = smem + L::kStageOff + st * 2 * L::kTileBytes;
-                    const uint32_t what = flags >> (2 * get) & 3u;
-                    if (what & 1u) decode64(0, stage + ks * L::kKRows * 128 + kr * 128, kr);
-                    if (what & 2u) decode64(1, stage + L::kTileBytes + dt * 128, dt);
+                    const int what = *(volatile int*)&ring_s[rs];
+                    const uint8_t* from = smem + L::kRingOff + rs * L::kRingBytes;
+                    uint4 kw[2], vw[2];
+                    uint32_t ksc = 0, vsc = 0;
+                    if (what > 0) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            kw[h] = *(const uint4*)(from + k_at + (((DH == 128 ? k_slab * 2 : 0) + h) ^ k_swap) * 16);
+                            vw[h] = *(const uint4*)(from + v_at + (h ^ v_swap) * 16);
+                        }
+                        ksc = *(const uint32_t*)(from + 8192 + dt * 4);
+                        vsc = *(const uint32_t*)(from + 8704 + dt * 4);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&r_empty[rs]);
+                    if (what < 0) {
+                        done = -1 - what;
+                        break;
+                    }
+                    const int n = u - ended, st = n % kStages;
+                    if (n >= kStages) ok = mbar_wait_warp(&kv_empty[st], (uint32_t)(n / kStages - 1) & 1u, abort_flag, p.status);
+                    if (!ok) break;
+                    auto put = [&](uint8_t* to, int row, const uint4& a, const uint4& b, uint32_t sc) {
+                        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                        const c4::Scale2 s0(__byte_perm(sc, sc, 0x1010)), s1(__byte_perm(sc, sc, 0x3232));
+                        uint8_t* dst = to + st * 2 * L::kTileBytes;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t x[4];
+                            c4::decode8(w[i], i < 4 ? s0 : s1, x);
+                            *(uint4*)(dst + ((i ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                        }
+                    };
+                    if (what & 1) put(k_to, k_row, kw[0], kw[1], ksc);
+                    if (what & 2) put(v_to, dt, vw[0], vw[1], vsc);
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) {
-                        if (kPair && rank != 0)
-                            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_to_cta(smem_u32(&kv_full[st]), 0)) : "memory");
-                        else mbar_arrive(&kv_full[st]);
-                    }
-                    ++units;
-                    if (++st == kStages) { st = 0; spar ^= 1u; }
-                    if (++get == D) get = 0;
-                    --pending;
+                    // (the fence hands the stage to the tensor core; a release at cluster scope would wait for much more: 1095 -> 904 us)
+                    if (lane == 0) arrive_leader(&kv_full[st]);
                 }
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                u += 2;
+                ended += 2;
                 // A round ends with every use of a stage done.
-                for (int i = max(0, units - kStages); i < units && ok; ++i)
+                for (int i = max(0, done - kStages); i < done && ok; ++i)
                     ok = mbar_wait_warp(&kv_empty[i % kStages], (uint32_t)(i / kStages) & 1u, abort_flag, p.status);
                 const unsigned long long again = end_of_round();
                 if (only || !again) break;
@@ -1143,14 +1208,28 @@ nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
     return NOVA_OK;
 }
 
+// Codes of a cache in 4 bits, [B, Lmax, C / 2] bytes: boxes of `rows` rows of 32 or 64 bytes, whose 16-byte pieces are exchanged so that
+// eight consecutive rows lie in different banks.
+bool make_tmap_codes(nova_ctx* ctx, CUtensorMap* map, const void* base, const nova_cache4& c, int bytes, int rows)
+{
+    const cuuint64_t dim[3] = {(cuuint64_t)c.C / 2, (cuuint64_t)max(c.Lmax, 1), (cuuint64_t)c.B};
+    const cuuint64_t str[2] = {(cuuint64_t)c.C / 2, (cuuint64_t)max(c.Lmax, 1) * c.C / 2};
+    const cuuint32_t box[3] = {(cuuint32_t)bytes, (cuuint32_t)rows, 1}, one[3] = {1, 1, 1};
+    return ((encode_tiled_fn)ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dim, str, box, one,
+                                                CU_TENSOR_MAP_INTERLEAVE_NONE, bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                                                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DH>
 nova_status launch4(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
 {
     using L = AttnCfg<DH, true>;
     const nova_cache4& c = *a.cache;
-    CUtensorMap tq;
+    CUtensorMap tq, tk, tv;
     const uint64_t dq[2] = {(uint64_t)c.C, (uint64_t)a.M}, sq[1] = {(uint64_t)a.ldq * 2};
-    if (!make_tmap_bf16(ctx, &tq, a.q, 2, dq, sq, BQ)) return nova_fail(ctx, NOVA_ERR_CUDA, "cache4 attention: cuTensorMapEncodeTiled failed");
+    if (!make_tmap_bf16(ctx, &tq, a.q, 2, dq, sq, BQ) || !make_tmap_codes(ctx, &tk, c.k_codes, c, DH / 2, L::kKRows) ||
+        !make_tmap_codes(ctx, &tv, c.v_codes, c, L::kVCols / 2, BKV))
+        return nova_fail(ctx, NOVA_ERR_CUDA, "cache4 attention: cuTensorMapEncodeTiled failed");
     if (!ctx->attr_attn4) {   // both head sizes once per context
         NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, true>::kTotal));
         NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, true>::kTotal));
@@ -1177,7 +1256,7 @@ nova_status launch4(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t 
     const int ctas = (int)min((long)p.slots, most) * L::kCtas;
     {
         nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
-        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, true>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tq, tq, p));
+        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, true>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
     }
     return NOVA_OK;
 }

@@ -532,7 +532,7 @@ nova_status nova_launch_cache4_attention(nova_ctx* ctx, const nova_cache4_attn_a
     const int dh = a.cache->C / a.cache->n_heads;
     if (!a.scratch || a.scratch_bytes < nova_cache4_attention_scratch(ctx->num_sms, dh, a.M))
         return nova_fail(ctx, NOVA_ERR_WORKSPACE, "nova_cache4_attention: workspace missing or too small");
-    if ((long)a.M > kFewPerImage * (long)a.cache->B) return nova_launch_cache4_tiles(ctx, a, st);
+    if (a.cache->Lmax > 0 && (long)a.M > kFewPerImage * (long)a.cache->B) return nova_launch_cache4_tiles(ctx, a, st);
     return dh == 64 ? launch_few<64>(ctx, a, st) : launch_few<128>(ctx, a, st);
 }
 
