@@ -41,6 +41,8 @@
 // 300 x 821: 22.8 -> 12.5; 4 x 563 x 1779, 30 heads x 64: 80 -> 55; 2 x 128 x 552, 16 x 64: 11.8 -> 9.2.
 #include "cache4.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace tc;
@@ -270,8 +272,9 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     }
     int item = entry, khalf = -1, slot = 0;
     if (item >= whole) {
-        slot = Q4 ? (item - whole) / max_parts : (item - whole) >> 1;
-        khalf = Q4 ? (item - whole) - slot * max_parts : (item - whole) & 1;
+        // (Q4: first parts first, as an item may have fewer than there is room for)
+        slot = Q4 ? (item - whole) % rem : (item - whole) >> 1;
+        khalf = Q4 ? (item - whole) / rem : (item - whole) & 1;
         item = whole + slot;
     }
     const int head = item / units;
@@ -684,25 +687,50 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     // threads themselves hold up their fences and arrivals; with the codes copied here in pieces of 16 bytes the
                     // two warps needed 0.75 us per tile.)
                     const int lt = threadIdx.x - 64;
-                    int lead = kBufs, vi = next_pass(0, only), vj = 0, vpass = only ? 0 : 1, ends = 0;
                     bool ok = true;
                     const int scale_row = p.C >> 4;
-                    auto copy_scales = [&](uint32_t dst, const uint8_t* src, bool live) {
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
+                    // The cursors' tiles are kept in registers: read from the table each time, they were most of an iteration.
+                    int k_y = 0, k_last = 0, k_x = 0, k_b = 0, v_y = 0, v_last = 0, v_x = 0, v_b = 0;
+                    const uint8_t *k_sc = nullptr, *v_sc = nullptr;        // this thread's first scales of row 0 of the image
+                    auto enter_k = [&]() {
+                        if (si >= kTable) return;
+                        const Pass& t = table[si];
+                        k_y = t.first; k_last = t.last; k_x = t.x >> 1; k_b = t.b;
+                        k_sc = p.k_scales + ((long)t.b * p.Lmax + lt) * scale_row + (t.x >> 4);
+                    };
+                    int lead = kBufs, vi = next_pass(0, only), v_left = 0, vpass = only ? 0 : 1, ends = 0;
+                    auto enter_v = [&]() {
+                        if (vi >= kTable) return;
+                        const Pass& t = table[vi];
+                        const int x = t.x + (int)rank * L::kVCols;
+                        v_left = t.n; v_y = t.first; v_last = t.last; v_x = x >> 1; v_b = t.b;
+                        v_sc = p.v_scales + ((long)t.b * p.Lmax + lt) * scale_row + (x >> 4);
+                    };
+                    enter_k();
+                    enter_v();
+                    auto copy_scales = [&](uint32_t dst, const uint8_t* row0, int y, int r, auto bytes) {
+                        const bool live = y + r >= 0;                      // rows before the first read as zeros
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(row0 + (long)(live ? y : -r) * scale_row),
+                                     "n"(decltype(bytes)::value), "r"(live ? decltype(bytes)::value : 0) : "memory");
                     };
                     while (ends < 2) {
-                        bool has_v = false;
-                        const int i = vi, j = vj;
                         const bool over = lead == 0 && vi >= kTable;
+                        bool has_v = false;
+                        int yv = 0, xv = 0, bv = 0;
+                        const uint8_t* sv = v_sc;
                         if (lead > 0) --lead;
                         else if (!over) {
                             has_v = vpass == 1;
-                            if (++vj == table[vi].n) {
-                                vj = 0;
+                            yv = v_left == 1 ? v_last : v_y;
+                            xv = v_x;
+                            bv = v_b;
+                            v_y += BKV;
+                            if (--v_left == 0) {
                                 if (++vpass == 2) {
                                     vpass = only ? 0 : 1;
                                     vi = next_pass(vi + 1, only);
                                 }
+                                enter_v();
                             }
                         }
                         const bool has_k = s_left > 0;
@@ -710,34 +738,32 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         if (units >= L::kRing) ok = mbar_wait_warp(&r_empty[rs], rpar ^ 1u, abort_flag, p.status);
                         if (!ok) break;
                         uint8_t* const to = smem + L::kRingOff + rs * L::kRingBytes;
-                        const int si_now = si, yk = !has_k ? 0 : (s_left == 1 ? table[si].last : table[si].first + (s_n - s_left) * BKV) + (int)rank * L::kKRows;
-                        const int yv = !has_v ? 0 : j == table[i].n - 1 ? table[i].last : table[i].first + j * BKV;
-                        if (has_k) s_step();
+                        const uint32_t to_s = smem_u32(to) + 8192u;
+                        const int yk = (s_left == 1 ? k_last : k_y) + (int)rank * L::kKRows;
                         if (warp == 2 && elect_one()) {
                             ring_s[rs] = over ? -1 - stages : (has_k ? 1 : 0) | (has_v ? 2 : 0);
                             mbar_arrive_expect_tx(&r_full[rs], (has_k ? 4096 : 0) + (has_v ? 4096 : 0));
                             // (rows before the first read as zeros)
-                            if (has_k) tma_load_3d(to, &tmap_k, &r_full[rs], table[si_now].x >> 1, yk, table[si_now].b);
-                            if (has_v) tma_load_3d(to + 4096, &tmap_v, &r_full[rs], (table[i].x + (int)rank * L::kVCols) >> 1, yv, table[i].b);
+                            if (has_k) tma_load_3d(to, &tmap_k, &r_full[rs], k_x, yk, k_b);
+                            if (has_v) tma_load_3d(to + 4096, &tmap_v, &r_full[rs], xv, yv, bv);
                         }
                         __syncwarp();
                         if (has_k) {
-                            const uint8_t* scales = p.k_scales + (long)table[si_now].b * p.Lmax * scale_row + (table[si_now].x >> 4);
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const int at = c * 64 + lt, r = at / (DH / 64), sl = at % (DH / 64);
-                                copy_scales(smem_u32(to) + (uint32_t)(8192 + (sl * L::kKRows + r) * 4), scales + (long)max(yk + r, 0) * scale_row + sl * 4, yk + r >= 0);
+                            if constexpr (DH == 128) copy_scales(to_s + lt * 8, k_sc, yk, lt, std::integral_constant<int, 8>());
+                            else {
+                                copy_scales(to_s + lt * 4, k_sc, yk, lt, std::integral_constant<int, 4>());
+                                copy_scales(to_s + lt * 4 + 256, k_sc + 64 * scale_row, yk, lt + 64, std::integral_constant<int, 4>());
                             }
                         }
                         if (has_v) {
-                            const uint8_t* scales = p.v_scales + (long)table[i].b * p.Lmax * scale_row + ((table[i].x + (int)rank * L::kVCols) >> 4);
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const int r = c * 64 + lt;
-                                copy_scales(smem_u32(to) + (uint32_t)(8704 + r * 4), scales + (long)max(yv + r, 0) * scale_row, yv + r >= 0);
-                            }
+                            copy_scales(to_s + 512 + lt * 4, sv, yv, lt, std::integral_constant<int, 4>());
+                            copy_scales(to_s + 768 + lt * 4, sv + 64 * scale_row, yv, lt + 64, std::integral_constant<int, 4>());
                         }
                         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[rs])) : "memory");
+                        if (has_k) {
+                            k_y += BKV;
+                            if (s_step()) enter_k();
+                        }
                         ++units;
                         if (over) ++ends;              // (one for each of the two warpgroups that take turns)
                         else ++stages;
@@ -1095,37 +1121,37 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         // the exchange of 16-byte pieces in the ring: of rows of 64 bytes by (row / 2) mod 4, of 32 bytes by (row / 4) mod 2
         const int k_at = DH == 128 ? k_row * 64 : k_row * 32, k_swap = DH == 128 ? k_row >> 1 & 3 : k_row >> 2 & 1;
         const int v_at = 4096 + dt * 32, v_swap = dt >> 2 & 1;
-        int u = (warp - 16) >> 2, ended = 0;               // ring entry, ends of rounds among those before it
+        const int turn = (warp - 16) >> 2;
+        int rs = turn, st = turn, n = turn;                // ring entry, stage, stages so far; every other one
+        uint32_t rpar = 0, spar = 1;                       // phases of the two
+        auto next_ring = [&]() { if ((rs += 2) >= L::kRing) { rs -= L::kRing; rpar ^= 1u; } };
+        static_assert(kStages == 3 && kBufs <= kStages, "a turn of two stages passes the last one at most once");
         for (int base = 0; begin_round(base); base += kTable) {
             unsigned long long only = 0;
             do {
                 bool ok = true;
                 int done = 0;
-                for (;; u += 2) {
-                    const int rs = u % L::kRing;
-                    ok = mbar_wait_warp(&r_full[rs], (uint32_t)(u / L::kRing) & 1u, abort_flag, p.status);
+                while (true) {
+                    ok = mbar_wait_warp(&r_full[rs], rpar, abort_flag, p.status);
                     if (!ok) break;
-                    const int what = *(volatile int*)&ring_s[rs];
                     const uint8_t* from = smem + L::kRingOff + rs * L::kRingBytes;
+                    const int what = *(volatile int*)&ring_s[rs];
                     uint4 kw[2], vw[2];
-                    uint32_t ksc = 0, vsc = 0;
-                    if (what > 0) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            kw[h] = *(const uint4*)(from + k_at + (((DH == 128 ? k_slab * 2 : 0) + h) ^ k_swap) * 16);
-                            vw[h] = *(const uint4*)(from + v_at + (h ^ v_swap) * 16);
-                        }
-                        ksc = *(const uint32_t*)(from + 8192 + dt * 4);
-                        vsc = *(const uint32_t*)(from + 8704 + dt * 4);
+                    for (int h = 0; h < 2; ++h) {
+                        kw[h] = *(const uint4*)(from + k_at + (((DH == 128 ? k_slab * 2 : 0) + h) ^ k_swap) * 16);
+                        vw[h] = *(const uint4*)(from + v_at + (h ^ v_swap) * 16);
                     }
+                    const uint32_t ksc = *(const uint32_t*)(from + 8192 + (DH == 128 ? k_row * 8 + k_slab * 4 : dt * 4));
+                    const uint32_t vsc = *(const uint32_t*)(from + 8704 + dt * 4);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&r_empty[rs]);
+                    next_ring();
                     if (what < 0) {
                         done = -1 - what;
                         break;
                     }
-                    const int n = u - ended, st = n % kStages;
-                    if (n >= kStages) ok = mbar_wait_warp(&kv_empty[st], (uint32_t)(n / kStages - 1) & 1u, abort_flag, p.status);
+                    if (n >= kStages) ok = mbar_wait_warp(&kv_empty[st], spar, abort_flag, p.status);
                     if (!ok) break;
                     auto put = [&](uint8_t* to, int row, const uint4& a, const uint4& b, uint32_t sc) {
                         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -1144,9 +1170,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     __syncwarp();
                     // (the fence hands the stage to the tensor core; a release at cluster scope would wait for much more: 1095 -> 904 us)
                     if (lane == 0) arrive_leader(&kv_full[st]);
+                    n += 2;
+                    if ((st += 2) >= kStages) { st -= kStages; spar ^= 1u; }
                 }
-                u += 2;
-                ended += 2;
                 // A round ends with every use of a stage done.
                 for (int i = max(0, done - kStages); i < done && ok; ++i)
                     ok = mbar_wait_warp(&kv_empty[i % kStages], (uint32_t)(i / kStages) & 1u, abort_flag, p.status);
