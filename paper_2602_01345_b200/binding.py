@@ -103,8 +103,13 @@ def _ptr(t):
     return t.data_ptr() if t.numel() > 0 else None
 
 
+_raw_stream, _get_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None and _get_device is not None:      # 0.3 us; the object that current_stream makes takes 3.4
+            return _raw_stream(_get_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -763,6 +768,7 @@ class Cache4:
         self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.kv_len = k_codes, v_codes, k_scales, v_scales, kv_len
         self.B, self.Lmax, self.C, self.n_heads = B, Lmax, Cc, int(n_heads)
         self.c = _Cache4(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), _ptr(kv_len), B, Lmax, Cc, self.n_heads)
+        self.ref = C.byref(self.c)
 
     @classmethod
     def empty(cls, B: int, Lmax: int, C: int, n_heads: int, device="cuda:0"):
@@ -774,67 +780,66 @@ class Cache4:
 
 
 def _rows4(cache: Cache4, t):
-    """Checks compacted rows [M, C] (rows may lie apart, as slices of a wider tensor do) and gives their row stride."""
-    assert t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[1] == cache.C and t.stride(1) == 1, "rows must be bf16 [M, C]"
-    return t.stride(0) if t.shape[0] > 1 else cache.C
+    """Checks compacted rows [M, C] (rows may lie apart, as slices of a wider tensor do) and gives M and their row stride."""
+    shape, stride = t.shape, t.stride()
+    assert t.dtype is torch.bfloat16 and len(shape) == 2 and shape[1] == cache.C and stride[1] == 1, "rows must be bf16 [M, C]"
+    return shape[0], (stride[0] if shape[0] > 1 else cache.C)
 
 
-def _same_device4(ctx: Context, cache: Cache4, *tensors):
-    for t in (cache.kv_len,) + tensors:
-        assert t is None or (t.is_cuda and t.device.index == ctx.device), "tensors must lie on the context's device"
+def _on4(ctx: Context, *tensors):
+    """Pointers of tensors (None: null) that have to lie on the context's device."""
+    for t in tensors:
+        assert t is None or t.get_device() == ctx.device, "tensors must lie on the context's device"
+    return [t.data_ptr() if t is not None else None for t in tensors]
 
 
 def _cu4(cache: Cache4, cu):
-    assert cu.dtype == torch.int32 and cu.numel() == cache.B + 1, "cu must be int32 [B + 1]"
-    return _ptr(cu)
+    assert cu.dtype is torch.int32 and cu.numel() == cache.B + 1 and cu.is_contiguous(), "cu must be int32 [B + 1]"
+    return cu
 
 
 def nova_cache4_workspace_bytes(ctx: Context, cache: Cache4, M: int) -> int:
-    return int(_lib.nova_cache4_workspace_bytes(ctx.handle, C.byref(cache.c), M))
+    return int(_lib.nova_cache4_workspace_bytes(ctx.handle, cache.ref, M))
 
 
 def nova_cache4_append(ctx: Context, cache: Cache4, k, v, cu_rows, advance: bool = True, stream=None):
     """Rounds the rows of k and v (bf16 [M, C], image b's at cu_rows[b] .. cu_rows[b+1]-1) to 4 bits and writes them behind
     the cache's rows; advance: kv_len then counts them."""
-    M, ld = k.shape[0], _rows4(cache, k)
-    assert v.shape == k.shape and _rows4(cache, v) == ld, "k and v must have one layout"
-    _same_device4(ctx, cache, k, v, cu_rows)
-    ctx.check(_lib.nova_cache4_append(ctx.handle, C.byref(cache.c), k.data_ptr() if M else None, v.data_ptr() if M else None, ld,
-                                      _cu4(cache, cu_rows), M, int(bool(advance)), _stream(stream)))
+    M, ld = _rows4(cache, k)
+    assert _rows4(cache, v) == (M, ld), "k and v must have one layout"
+    _, kp, vp, cp = _on4(ctx, cache.kv_len, k, v, _cu4(cache, cu_rows))
+    ctx.check(_lib.nova_cache4_append(ctx.handle, cache.ref, kp, vp, ld, cp, M, 1 if advance else 0, _stream(stream)))
 
 
 def nova_cache4_read(ctx: Context, cache: Cache4, cu_rows, k_out, v_out, first=None, stream=None):
     """Cache rows first[b] .. (int32 [B]; None: from row 0), cu_rows[b+1] - cu_rows[b] of them, as bf16 to rows cu_rows[b] .. of
     k_out and v_out [M, C]."""
-    M, ld = k_out.shape[0], _rows4(cache, k_out)
-    assert v_out.shape == k_out.shape and _rows4(cache, v_out) == ld, "k_out and v_out must have one layout"
-    assert first is None or (first.dtype == torch.int32 and first.numel() == cache.B)
-    _same_device4(ctx, cache, k_out, v_out, cu_rows, first)
-    ctx.check(_lib.nova_cache4_read(ctx.handle, C.byref(cache.c), _ptr(first), _cu4(cache, cu_rows), M, k_out.data_ptr() if M else None,
-                                    v_out.data_ptr() if M else None, ld, _stream(stream)))
+    M, ld = _rows4(cache, k_out)
+    assert _rows4(cache, v_out) == (M, ld), "k_out and v_out must have one layout"
+    assert first is None or (first.dtype is torch.int32 and first.numel() == cache.B and first.is_contiguous())
+    _, kp, vp, cp, fp = _on4(ctx, cache.kv_len, k_out, v_out, _cu4(cache, cu_rows), first)
+    ctx.check(_lib.nova_cache4_read(ctx.handle, cache.ref, fp, cp, M, kp, vp, ld, _stream(stream)))
 
 
 def nova_cache4_attention(ctx: Context, cache: Cache4, q, cu_q, o, lse=None, stream=None):
     """o [M, C] bf16 = attention of the queries q [M, C] (image b's at cu_q[b] .. cu_q[b+1]-1) over the cache's rows; lse f32
     [n_heads, M] or None: the log-sum-exp of every query's scores. Needs a workspace (Context.ensure_cache4_workspace)."""
-    M, ld = q.shape[0], _rows4(cache, q)
-    assert o.dtype == torch.bfloat16 and o.shape == q.shape
-    assert lse is None or (lse.dtype == torch.float32 and lse.shape == (cache.n_heads, M))
-    _same_device4(ctx, cache, q, cu_q, o, lse)
-    ctx.check(_lib.nova_cache4_attention(ctx.handle, C.byref(cache.c), q.data_ptr() if M else None, ld, _cu4(cache, cu_q), M, _ptr(o),
-                                         _ptr(lse), _stream(stream)))
+    M, ld = _rows4(cache, q)
+    assert o.dtype is torch.bfloat16 and o.shape == q.shape and o.is_contiguous()
+    assert lse is None or (lse.dtype is torch.float32 and lse.shape == (cache.n_heads, M) and lse.is_contiguous())
+    _, qp, cp, op, lp = _on4(ctx, cache.kv_len, q, _cu4(cache, cu_q), o, lse)
+    ctx.check(_lib.nova_cache4_attention(ctx.handle, cache.ref, qp, ld, cp, M, op, lp, _stream(stream)))
 
 
 def nova_cache4_weights(ctx: Context, cache: Cache4, q, lse, cu_q, weight_out, weight_in=None, stream=None):
     """weight_out [B, Lmax] f32 = weight_in (None: zeros; may be weight_out itself) + the attention weight that each cached row
     receives from these queries, given the log-sum-exp that nova_cache4_attention left."""
-    M, ld = q.shape[0], _rows4(cache, q)
-    assert lse.dtype == torch.float32 and lse.shape == (cache.n_heads, M)
+    M, ld = _rows4(cache, q)
+    assert lse.dtype is torch.float32 and lse.shape == (cache.n_heads, M) and lse.is_contiguous()
     for t in (weight_in, weight_out):
-        assert t is None or (t.dtype == torch.float32 and t.shape == (cache.B, cache.Lmax))
-    _same_device4(ctx, cache, q, lse, cu_q, weight_out, weight_in)
-    ctx.check(_lib.nova_cache4_weights(ctx.handle, C.byref(cache.c), q.data_ptr() if M else None, ld, _ptr(lse), _cu4(cache, cu_q), M,
-                                       _ptr(weight_in), _ptr(weight_out), _stream(stream)))
+        assert t is None or (t.dtype is torch.float32 and t.shape == (cache.B, cache.Lmax) and t.is_contiguous())
+    _, qp, lp, cp, op, ip = _on4(ctx, cache.kv_len, q, lse, _cu4(cache, cu_q), weight_out, weight_in)
+    ctx.check(_lib.nova_cache4_weights(ctx.handle, cache.ref, qp, ld, lp, cp, M, ip, op, _stream(stream)))
 
 
 def nova_cache4_evict(ctx: Context, cache: Cache4, weight, budget: int, recent: int, dst: Cache4, weight_out=None, src_row=None,
@@ -842,9 +847,8 @@ def nova_cache4_evict(ctx: Context, cache: Cache4, weight, budget: int, recent: 
     """Writes to dst the cache's last `recent` rows and the highest-weighted of the others, `budget` in all per image, in their
     order. weight f32 [B, Lmax]; weight_out f32 [B, dst.Lmax] or None; src_row int32 [B, budget] or None (then the workspace
     holds the list)."""
-    assert weight.dtype == torch.float32 and weight.shape == (cache.B, cache.Lmax)
-    assert weight_out is None or (weight_out.dtype == torch.float32 and weight_out.shape == (dst.B, dst.Lmax))
-    assert src_row is None or (src_row.dtype == torch.int32 and src_row.shape == (cache.B, budget))
-    _same_device4(ctx, cache, weight, dst.kv_len, weight_out, src_row)
-    ctx.check(_lib.nova_cache4_evict(ctx.handle, C.byref(cache.c), _ptr(weight), budget, recent, C.byref(dst.c), _ptr(weight_out),
-                                     _ptr(src_row), _stream(stream)))
+    assert weight.dtype is torch.float32 and weight.shape == (cache.B, cache.Lmax) and weight.is_contiguous()
+    assert weight_out is None or (weight_out.dtype is torch.float32 and weight_out.shape == (dst.B, dst.Lmax) and weight_out.is_contiguous())
+    assert src_row is None or (src_row.dtype is torch.int32 and src_row.shape == (cache.B, budget) and src_row.is_contiguous())
+    _, wp, _, op, rp = _on4(ctx, cache.kv_len, weight, dst.kv_len, weight_out, src_row)
+    ctx.check(_lib.nova_cache4_evict(ctx.handle, cache.ref, wp, budget, recent, dst.ref, op, rp, _stream(stream)))

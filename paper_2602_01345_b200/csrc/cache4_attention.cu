@@ -37,7 +37,8 @@ struct FewCfg {
     static constexpr int kRedBytes = (kWarps + 1) / 2 * kFewRows * DH * 4;       // accumulators of half of the warps
     static constexpr int kRingOff = kRedBytes;
     static constexpr int kStatOff = kRingOff + kWarps * kDepth * kStageBytes;    // [kWarps][16] maxima and sums
-    static constexpr int kTotal = kStatOff + kWarps * kFewRows * 8;
+    static constexpr int kQOff = kStatOff + kWarps * kFewRows * 8;               // Q as the lanes take it: [steps / 2][rows g, g + 8][lane] x 16 bytes
+    static constexpr int kTotal = kQOff + DH / 32 * 2 * 32 * 16;
     static constexpr int kSlotFloats = kFewRows * (DH + 2);   // a partial result: O, maxima, sums
 };
 
@@ -185,31 +186,61 @@ cache4_few_kernel(const FewParams p)
     pf.seek(p, first);
     FewWalk<DH> at = pf;
     long issued = first;
+    // Copies: a lane's pieces of a tile lie a constant number of rows apart; its place in the image and head is kept.
+    constexpr int kPieces = L::kRowBytes / 16, kRowsApart = 32 / kPieces;
+    const int code_row = p.C / 2, scale_row = p.C / 16, my_n = lane / kPieces;
+    const long v_codes_at = p.v_codes - p.k_codes, v_scales_at = p.v_scales - p.k_scales;
+    const uint8_t *code_at, *scale_at;
+    uint32_t k_dst[kPieces], v_dst[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int n = i * kRowsApart + my_n, c = lane % kPieces, vr = v_row(n);
+        k_dst[i] = (uint32_t)(n * L::kRowBytes + c * 16);
+        v_dst[i] = kVOff + (uint32_t)(vr * L::kRowBytes + (c ^ v_swap(vr)) * 16);
+    }
+    const uint32_t ring_s = tc::smem_u32(ring);
+    auto enter = [&]() {
+        const int head = pf.unit % p.n_heads;
+        const long row = (long)pf.b * p.Lmax + warp * kWarpKeys;
+        code_at = p.k_codes + (row + my_n) * code_row + head * L::kRowBytes + lane % kPieces * 16;
+        scale_at = p.k_scales + (row + lane) * scale_row + head * L::kScaleBytes;
+    };
+    enter();
     auto issue = [&](int slot) {
         if (issued < end) {
-            const int key0 = pf.t * L::kTile + warp * kWarpKeys;
-            if (pf.len > key0) {
-                const uint32_t s = tc::smem_u32(ring + slot * L::kStageBytes);
-                const int head = pf.unit % p.n_heads;
-                const long base = (long)pf.b * p.Lmax;
-                constexpr int kPieces = L::kRowBytes / 16;
+            const int tile0 = pf.t * L::kTile, left = pf.len - tile0 - warp * kWarpKeys;       // keys from this warp's first on
+            if (left > 0) {
+                const uint32_t to = ring_s + (uint32_t)(slot * L::kStageBytes);
+                const uint8_t* src = code_at + (long)tile0 * code_row;
+                const uint8_t* sc = scale_at + (long)tile0 * scale_row;
+                if (left >= kWarpKeys) {
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int n = (i * 32 + lane) / kPieces, c = (i * 32 + lane) % kPieces;
-                    const bool live = key0 + n < pf.len;
-                    const long row = base + min(key0 + n, pf.len - 1);
-                    const long src = row * (p.C / 2) + head * L::kRowBytes + c * 16;
-                    cp_async16(s + (uint32_t)(n * L::kRowBytes + c * 16), p.k_codes + src, live);
-                    const int vr = v_row(n);
-                    cp_async16(s + kVOff + (uint32_t)(vr * L::kRowBytes + (c ^ v_swap(vr)) * 16), p.v_codes + src, live);
+                    for (int i = 0; i < kPieces; ++i) {
+                        cp_async16(to + k_dst[i], src, true);
+                        cp_async16(to + v_dst[i], src + v_codes_at, true);
+                        src += kRowsApart * code_row;
+                    }
+                    cp_async_small<L::kScaleBytes>(to + kKsOff + (uint32_t)(lane * L::kScaleBytes), sc, true);
+                    cp_async_small<L::kScaleBytes>(to + kVsOff + (uint32_t)(lane * L::kScaleBytes), sc + v_scales_at, true);
+                } else {
+                    // (what lies past the last key reads as zeros; its address is that of row 0 of the tile)
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const bool live = i * kRowsApart + my_n < left;
+                        const uint8_t* at = live ? src + (long)(i * kRowsApart) * code_row : src - (long)my_n * code_row;
+                        cp_async16(to + k_dst[i], at, live);
+                        cp_async16(to + v_dst[i], at + v_codes_at, live);
+                    }
+                    const bool live = lane < left;
+                    if (!live) sc -= (long)lane * scale_row;
+                    cp_async_small<L::kScaleBytes>(to + kKsOff + (uint32_t)(lane * L::kScaleBytes), sc, live);
+                    cp_async_small<L::kScaleBytes>(to + kVsOff + (uint32_t)(lane * L::kScaleBytes), sc + v_scales_at, live);
                 }
-                const bool live = key0 + lane < pf.len;
-                const long src = (base + min(key0 + lane, pf.len - 1)) * (p.C / 16) + head * L::kScaleBytes;
-                cp_async_small<L::kScaleBytes>(s + kKsOff + (uint32_t)(lane * L::kScaleBytes), p.k_scales + src, live);
-                cp_async_small<L::kScaleBytes>(s + kVsOff + (uint32_t)(lane * L::kScaleBytes), p.v_scales + src, live);
             }
             ++issued;
+            const long unit_at = pf.row0;
             pf.next(p, issued < end);
+            if (pf.row0 != unit_at) enter();
         }
         cp_commit();
     };
@@ -217,6 +248,7 @@ cache4_few_kernel(const FewParams p)
     for (int i = 0; i < L::kDepth - 1; ++i) issue(i);
 
     float* stat = (float*)(smem + L::kStatOff);
+    uint4* q_s = (uint4*)(smem + L::kQOff);
     int slot = 0;
     for (long tile = first; tile < end;) {
         // ---- a piece: the tiles of one unit that are this CTA's
@@ -224,21 +256,14 @@ cache4_few_kernel(const FewParams p)
         const int row_base = p.cu[at.b] + q0, rows = min(at.rows - q0, kFewRows), len = at.len;
         const long row0 = at.row0;
         const int T = at.T;
-        // Q: channels t * DH/4 .. of rows g and g + 8
-        uint32_t qa[kSteps][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        // Q: channels t * DH/4 .. of rows g and g + 8, for all warps
+        if (threadIdx.x < kSteps / 2 * 64) {
+            const int h = (threadIdx.x >> 5) & 1, i = threadIdx.x >> 6;
             const bool live = g + 8 * h < rows && row_base + g + 8 * h < p.M;
             const uint4* src = (const uint4*)(p.q + (long)(row_base + (live ? g + 8 * h : 0)) * p.ldq + head * DH + t * (DH / 4));
-#pragma unroll
-            for (int i = 0; i < kSteps / 2; ++i) {
-                const uint4 v = live ? src[i] : make_uint4(0, 0, 0, 0);
-                qa[2 * i][h] = v.x;
-                qa[2 * i][2 + h] = v.y;
-                qa[2 * i + 1][h] = v.z;
-                qa[2 * i + 1][2 + h] = v.w;
-            }
+            q_s[threadIdx.x] = live ? src[i] : make_uint4(0, 0, 0, 0);
         }
+        __syncthreads();
         float acc[kBlocks][4];
 #pragma unroll
         for (int j = 0; j < kBlocks; ++j)
@@ -254,26 +279,30 @@ cache4_few_kernel(const FewParams p)
             if (key0 < len) {
                 const uint8_t* s_at = ring + slot * L::kStageBytes;
                 float s[4][4];
+                uint32_t kw[4][4], ks[4];
 #pragma unroll
                 for (int nb = 0; nb < 4; ++nb) {
                     s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
                     const int n = nb * 8 + g;
                     // dh 128: this thread's 32 channels are one group; dh 64: its 16 are half of one
-                    const Scale2 sc(both(*(const uint16_t*)(s_at + kKsOff + n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2)));
-                    uint32_t w[4];
+                    ks[nb] = both(*(const uint16_t*)(s_at + kKsOff + n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2));
                     if constexpr (DH == 128) {
                         const uint4 v = *(const uint4*)(s_at + n * L::kRowBytes + t * 16);
-                        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                        kw[nb][0] = v.x; kw[nb][1] = v.y; kw[nb][2] = v.z; kw[nb][3] = v.w;
                     } else {
                         const uint2 v = *(const uint2*)(s_at + n * L::kRowBytes + t * 8);
-                        w[0] = v.x; w[1] = v.y; w[2] = w[3] = 0;
+                        kw[nb][0] = v.x; kw[nb][1] = v.y;
                     }
+                }
 #pragma unroll
-                    for (int i = 0; i < kSteps / 2; ++i) {
+                for (int i = 0; i < kSteps / 2; ++i) {
+                    const uint4 a = q_s[i * 64 + lane], b = q_s[i * 64 + 32 + lane];
+#pragma unroll
+                    for (int nb = 0; nb < 4; ++nb) {
                         uint32_t x[4];
-                        decode8(w[i], sc, x);
-                        mma16816(s[nb], qa[2 * i][0], qa[2 * i][1], qa[2 * i][2], qa[2 * i][3], x[0], x[1]);
-                        mma16816(s[nb], qa[2 * i + 1][0], qa[2 * i + 1][1], qa[2 * i + 1][2], qa[2 * i + 1][3], x[2], x[3]);
+                        decode8(kw[nb][i], Scale2(ks[nb]), x);
+                        mma16816(s[nb], a.x, b.x, a.y, b.y, x[0], x[1]);
+                        mma16816(s[nb], a.z, b.z, a.w, b.w, x[2], x[3]);
                     }
                 }
                 if (key0 + kWarpKeys > len) {
@@ -512,7 +541,11 @@ nova_status launch_few(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream
     const long tiles = units * (c.Lmax / L::kTile + 1);
     const int ctas = (int)min(min((long)ctx->num_sms, (long)NOVA_TICKETS), tiles);
     static_assert(L::kTotal <= 227 * 1024, "shared memory");
-    NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(cache4_few_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal));
+    if (!ctx->attr_few) {
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(cache4_few_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<64>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(cache4_few_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewCfg<128>::kTotal));
+        ctx->attr_few = true;
+    }
     nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
     NOVA_CUDA_CHECK(ctx, nova_launch_pdl(cache4_few_kernel<DH>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, 0, p));
     return NOVA_OK;

@@ -117,7 +117,7 @@ def test_binding_refuses_wrong_tensors():
     for bad in (rows.float(), rows[:, :64], torch.zeros((3, 256), dtype=torch.bfloat16)[:, ::2], rows[0]):
         with pytest.raises(AssertionError):
             nv._rows4(c, bad)
-    assert nv._rows4(c, torch.zeros((3, 384), dtype=torch.bfloat16)[:, 128:256]) == 384
+    assert nv._rows4(c, torch.zeros((3, 384), dtype=torch.bfloat16)[:, 128:256]) == (3, 384)
     with pytest.raises(AssertionError):
         nv._cu4(c, cu.long())
     with pytest.raises(AssertionError):
