@@ -18,8 +18,9 @@ using namespace c4;
 constexpr int kWtWarps = 8, kWtThreads = kWtWarps * 32;
 constexpr int kWtKeys = 32;                       // per warp
 constexpr int kWtTile = kWtWarps * kWtKeys;
-constexpr int kWtChunk = 32;                      // queries in shared memory at a time
-constexpr int kWtDepth = 3;                       // chunks in flight
+constexpr int kWtChunk = 64;                      // queries in shared memory at a time
+constexpr int kWtDepth = 2;                       // chunks in flight
+constexpr int kWtWaves = 8;                       // CTAs per SM that the parts aim at
 
 struct WeightParams {
     const uint8_t *codes, *scales;
@@ -136,26 +137,31 @@ cache4_weights_kernel(const WeightParams p)
                 if (head * chunks + chunks < j1) load_k(head + 1);
             }
             const int slot = (j - j0) % kWtDepth;
+#pragma unroll 1
+            for (int nb = 0; nb < kWtChunk / 8; nb += 2) {       // 16 queries: four independent chains of products
+                float s[2][2][4];
 #pragma unroll
-            for (int nb = 0; nb < kWtChunk / 8; ++nb) {
-                float s[2][4];
-#pragma unroll
-                for (int mi = 0; mi < 2; ++mi) s[mi][0] = s[mi][1] = s[mi][2] = s[mi][3] = 0.f;
+                for (int k = 0; k < 8; ++k) s[k >> 2][(k >> 1) & 1][2 * (k & 1)] = s[k >> 2][(k >> 1) & 1][2 * (k & 1) + 1] = 0.f;
                 const int row = nb * 8 + g;
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint4 v = *(const uint4*)&q_s[slot][(row * kRowChunks + piece_at(row, t * (DH / 32) + i)) * 16];
 #pragma unroll
-                    for (int mi = 0; mi < 2; ++mi) {
-                        mma16816(s[mi], a[mi][2 * i], v.x, v.y);
-                        mma16816(s[mi], a[mi][2 * i + 1], v.z, v.w);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 v = *(const uint4*)&q_s[slot][((row + 8 * h) * kRowChunks + piece_at(row, t * (DH / 32) + i)) * 16];
+#pragma unroll
+                        for (int mi = 0; mi < 2; ++mi) mma16816(s[h][mi], a[mi][2 * i], v.x, v.y);
+#pragma unroll
+                        for (int mi = 0; mi < 2; ++mi) mma16816(s[h][mi], a[mi][2 * i + 1], v.z, v.w);
                     }
                 }
-                const float2 nl = *(const float2*)&lse_s[slot][nb * 8 + 2 * t];
 #pragma unroll
-                for (int mi = 0; mi < 2; ++mi) {
-                    acc[2 * mi] += ex2(fmaf(s[mi][0], p.scale_log2e, nl.x)) + ex2(fmaf(s[mi][1], p.scale_log2e, nl.y));
-                    acc[2 * mi + 1] += ex2(fmaf(s[mi][2], p.scale_log2e, nl.x)) + ex2(fmaf(s[mi][3], p.scale_log2e, nl.y));
+                for (int h = 0; h < 2; ++h) {
+                    const float2 nl = *(const float2*)&lse_s[slot][(nb + h) * 8 + 2 * t];
+#pragma unroll
+                    for (int mi = 0; mi < 2; ++mi) {
+                        acc[2 * mi] += ex2(fmaf(s[h][mi][0], p.scale_log2e, nl.x)) + ex2(fmaf(s[h][mi][1], p.scale_log2e, nl.y));
+                        acc[2 * mi + 1] += ex2(fmaf(s[h][mi][2], p.scale_log2e, nl.x)) + ex2(fmaf(s[h][mi][3], p.scale_log2e, nl.y));
+                    }
                 }
             }
         }
@@ -196,7 +202,7 @@ cache4_weights_kernel(const WeightParams p)
 
 }  // namespace
 
-size_t nova_cache4_weights_scratch(int num_sms) { return (size_t)num_sms * 2 * kWtTile * sizeof(float); }
+size_t nova_cache4_weights_scratch(int num_sms) { return (size_t)num_sms * kWtWaves * kWtTile * sizeof(float); }
 
 nova_status nova_launch_cache4_weights(nova_ctx* ctx, const nova_cache4* c, const __nv_bfloat16* q, int64_t ldq, const float* lse, const int32_t* cu,
                                        int M, const float* in, float* out, bool own_rows, void* scratch, size_t scratch_bytes, cudaStream_t st)
@@ -209,9 +215,10 @@ nova_status nova_launch_cache4_weights(nova_ctx* ctx, const nova_cache4* c, cons
     p.scale_log2e = (float)((1.0 / sqrt((double)dh)) * 1.4426950408889634);
     p.tiles = (c->Lmax + kWtTile - 1) / kWtTile;
     const long whole = (long)c->B * p.tiles;
-    // as many parts as bring the launch to two CTAs per SM, no more than there can be (head, chunk) pairs
+    // as many parts as bring the launch to kWtWaves CTAs per SM (two run at once; the images' lengths differ), no more than there can
+    // be (head, chunk) pairs
     const long pairs = (long)c->n_heads * (((long)M + kWtChunk - 1) / kWtChunk);
-    p.parts = (int)max(1l, min(pairs, 2l * ctx->num_sms / whole));
+    p.parts = (int)max(1l, min(pairs, (long)kWtWaves * ctx->num_sms / whole));
     if (whole * p.parts > 0x7fffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_weights: too many rows");
     if (p.parts > 1 && (!scratch || scratch_bytes < nova_cache4_weights_scratch(ctx->num_sms)))
         return nova_fail(ctx, NOVA_ERR_WORKSPACE, "nova_cache4_weights: workspace missing or too small");
