@@ -85,22 +85,25 @@ __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, bo
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// A place in the launch's tiles: tile t of unit (b, head, block), of which the image has `units`, with T tiles each.
+// A place in the launch's tiles: tile t of unit (b, head, block), of which the image has `units`, with T tiles each, the first of
+// which (t = 0) has no keys: key tile t - 1 otherwise. Without it CTAs whose tiles are many units of few keys ended late.
 template <int DH>
 struct FewWalk {
     int b, unit, units, t, T, rows, len;
     long row0;                         // first tile of the present unit, counted over the launch
 
+    // (an image without keys has none: its rows are written by fill_empty)
     __device__ __forceinline__ static int image_units(const FewParams& p, int b)
     {
-        return (max(p.cu[b + 1] - p.cu[b], 0) + kFewRows - 1) / kFewRows * p.n_heads;
+        return image_len(p, b) == 0 ? 0 : (max(p.cu[b + 1] - p.cu[b], 0) + kFewRows - 1) / kFewRows * p.n_heads;
     }
     __device__ __forceinline__ static int image_len(const FewParams& p, int b)
     {
         const int n = max(p.kv_len[b], 0) + (p.own_rows ? max(p.cu[b + 1] - p.cu[b], 0) : 0);
         return min(n, p.Lmax);
     }
-    __device__ __forceinline__ static int tiles(int len) { return max((len + FewCfg<DH>::kTile - 1) / FewCfg<DH>::kTile, 1); }
+    // Tiles of a unit, and one more for what it costs to begin and to end one.
+    __device__ __forceinline__ static int tiles(int len) { return (len + FewCfg<DH>::kTile - 1) / FewCfg<DH>::kTile + 1; }
     __device__ __forceinline__ static long image_work(const FewParams& p, int b) { return (long)image_units(p, b) * tiles(image_len(p, b)); }
     // Tiles of the launch; by a whole warp.
     __device__ __forceinline__ static long total(const FewParams& p)
@@ -158,6 +161,23 @@ struct FewWalk {
     }
 };
 
+// Rows of images without keys: o = 0, lse = -inf. By all warps of the launch.
+template <int DH>
+__device__ __forceinline__ void fill_empty(const FewParams& p)
+{
+    const int lane = threadIdx.x & 31, warps = gridDim.x * FewCfg<DH>::kWarps, me = blockIdx.x * FewCfg<DH>::kWarps + (threadIdx.x >> 5);
+    for (int base = 0; base < p.B; base += 32) {
+        uint32_t todo = __ballot_sync(0xffffffffu, base + lane < p.B && FewWalk<DH>::image_len(p, base + lane) == 0);
+        for (; todo; todo &= todo - 1) {
+            const int b = base + __ffs((int)todo) - 1;
+            for (int r = p.cu[b] + me; r < min(p.cu[b + 1], p.M); r += warps) {
+                for (int c = lane; c < p.C / 8; c += 32) ((uint4*)(p.o + (long)r * p.C))[c] = make_uint4(0, 0, 0, 0);
+                for (int h = lane; p.lse && h < p.n_heads; h += 32) p.lse[(long)h * p.M + r] = -INFINITY;
+            }
+        }
+    }
+}
+
 template <int DH>
 __global__ void __launch_bounds__(FewCfg<DH>::kThreads, 1)
 cache4_few_kernel(const FewParams p)
@@ -169,6 +189,7 @@ cache4_few_kernel(const FewParams p)
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    fill_empty<DH>(p);
     const long W = FewWalk<DH>::total(p);
     const long G = min((long)gridDim.x, W);
     if ((long)blockIdx.x >= G) return;
@@ -208,7 +229,7 @@ cache4_few_kernel(const FewParams p)
     enter();
     auto issue = [&](int slot) {
         if (issued < end) {
-            const int tile0 = pf.t * L::kTile, left = pf.len - tile0 - warp * kWarpKeys;       // keys from this warp's first on
+            const int tile0 = (pf.t - 1) * L::kTile, left = pf.t == 0 ? 0 : pf.len - tile0 - warp * kWarpKeys;       // keys from this warp's first on
             if (left > 0) {
                 const uint32_t to = ring_s + (uint32_t)(slot * L::kStageBytes);
                 const uint8_t* src = code_at + (long)tile0 * code_row;
@@ -244,7 +265,7 @@ cache4_few_kernel(const FewParams p)
         }
         cp_commit();
     };
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < L::kDepth - 1; ++i) issue(i);
 
     float* stat = (float*)(smem + L::kStatOff);
@@ -275,82 +296,79 @@ cache4_few_kernel(const FewParams p)
             issue(slot == 0 ? L::kDepth - 1 : slot - 1);
             cp_wait<L::kDepth - 1>();
             __syncwarp();
-            const int key0 = (int)(tile - row0) * L::kTile + warp * kWarpKeys;
-            if (key0 < len) {
+            const int key0 = (int)(tile - row0 - 1) * L::kTile + warp * kWarpKeys;
+            if (tile > row0 && key0 < len) {
                 const uint8_t* s_at = ring + slot * L::kStageBytes;
-                float s[4][4];
-                uint32_t kw[4][4], ks[4];
-#pragma unroll
-                for (int nb = 0; nb < 4; ++nb) {
-                    s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
-                    const int n = nb * 8 + g;
-                    // dh 128: this thread's 32 channels are one group; dh 64: its 16 are half of one
-                    ks[nb] = both(*(const uint16_t*)(s_at + kKsOff + n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2));
-                    if constexpr (DH == 128) {
-                        const uint4 v = *(const uint4*)(s_at + n * L::kRowBytes + t * 16);
-                        kw[nb][0] = v.x; kw[nb][1] = v.y; kw[nb][2] = v.z; kw[nb][3] = v.w;
-                    } else {
-                        const uint2 v = *(const uint2*)(s_at + n * L::kRowBytes + t * 8);
-                        kw[nb][0] = v.x; kw[nb][1] = v.y;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint4 a = q_s[i * 64 + lane], b = q_s[i * 64 + 32 + lane];
-#pragma unroll
-                    for (int nb = 0; nb < 4; ++nb) {
-                        uint32_t x[4];
-                        decode8(kw[nb][i], Scale2(ks[nb]), x);
-                        mma16816(s[nb], a.x, b.x, a.y, b.y, x[0], x[1]);
-                        mma16816(s[nb], a.z, b.z, a.w, b.w, x[2], x[3]);
-                    }
-                }
-                if (key0 + kWarpKeys > len) {
-#pragma unroll
-                    for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (key0 + nb * 8 + 2 * t + (e & 1) >= len) s[nb][e] = -INFINITY;
-                }
-                float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                for (int nb = 0; nb < 4; ++nb) {
-                    top[0] = fmaxf(top[0], fmaxf(s[nb][0], s[nb][1]));
-                    top[1] = fmaxf(top[1], fmaxf(s[nb][2], s[nb][3]));
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-                    top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2)) * p.scale_log2e;
-                }
-                if (__any_sync(0xffffffffu, top[0] > m[0] + kRescale || top[1] > m[1] + kRescale)) {
-                    float f[2];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float m_new = top[h] > m[h] + kRescale ? top[h] : m[h];
-                        f[h] = ex2(m[h] - m_new);
-                        m[h] = m_new;
-                        l[h] *= f[h];
-                    }
-#pragma unroll
-                    for (int j = 0; j < kBlocks; ++j) {
-                        acc[j][0] *= f[0]; acc[j][1] *= f[0];
-                        acc[j][2] *= f[1]; acc[j][3] *= f[1];
-                    }
-                }
-                uint32_t pa[2][4];
-#pragma unroll
-                for (int nb = 0; nb < 4; ++nb) {
-                    float e[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[nb][i], p.scale_log2e, -m[i >> 1]));
-                    l[0] += e[0] + e[1];
-                    l[1] += e[2] + e[3];
-                    pa[nb >> 1][(nb & 1) * 2] = pack_bf16(e[0], e[1]);
-                    pa[nb >> 1][(nb & 1) * 2 + 1] = pack_bf16(e[2], e[3]);
-                }
-#pragma unroll
+                // 16 keys at a time, in a loop that is not unrolled: the code is fetched once per launch, 16 KB in about 6 us
+                // (with 32 keys at a time, 68 KB of code in all, 47 us of a launch of 61 passed before the second tile)
+#pragma unroll 1
                 for (int kb = 0; kb < 2; ++kb) {
+                    if (key0 + 16 * kb >= len) break;
+                    float s[2][4];
+                    uint32_t kw[2][4], ks[2];
+#pragma unroll
+                    for (int nb = 0; nb < 2; ++nb) {
+                        s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+                        const int n = 16 * kb + nb * 8 + g;
+                        // dh 128: this thread's 32 channels are one group; dh 64: its 16 are half of one
+                        ks[nb] = both(*(const uint16_t*)(s_at + kKsOff + n * L::kScaleBytes + (DH == 128 ? t : t >> 1) * 2));
+                        if constexpr (DH == 128) {
+                            const uint4 v = *(const uint4*)(s_at + n * L::kRowBytes + t * 16);
+                            kw[nb][0] = v.x; kw[nb][1] = v.y; kw[nb][2] = v.z; kw[nb][3] = v.w;
+                        } else {
+                            const uint2 v = *(const uint2*)(s_at + n * L::kRowBytes + t * 8);
+                            kw[nb][0] = v.x; kw[nb][1] = v.y;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kSteps / 2; ++i) {
+                        const uint4 a = q_s[i * 64 + lane], b = q_s[i * 64 + 32 + lane];
+#pragma unroll
+                        for (int nb = 0; nb < 2; ++nb) {
+                            uint32_t x[4];
+                            decode8(kw[nb][i], Scale2(ks[nb]), x);
+                            mma16816(s[nb], a.x, b.x, a.y, b.y, x[0], x[1]);
+                            mma16816(s[nb], a.z, b.z, a.w, b.w, x[2], x[3]);
+                        }
+                    }
+                    if (key0 + 16 * kb + 16 > len) {
+#pragma unroll
+                        for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (key0 + 16 * kb + nb * 8 + 2 * t + (e & 1) >= len) s[nb][e] = -INFINITY;
+                    }
+                    float top[2];
+                    top[0] = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])) * p.scale_log2e;
+                    top[1] = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3])) * p.scale_log2e;
+                    if (__any_sync(0xffffffffu, top[0] > m[0] + kRescale || top[1] > m[1] + kRescale)) {
+                        float f[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+                            top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+                            const float m_new = top[h] > m[h] + kRescale ? top[h] : m[h];
+                            f[h] = ex2(m[h] - m_new);
+                            m[h] = m_new;
+                            l[h] *= f[h];
+                        }
+#pragma unroll
+                        for (int j = 0; j < kBlocks; ++j) {
+                            acc[j][0] *= f[0]; acc[j][1] *= f[0];
+                            acc[j][2] *= f[1]; acc[j][3] *= f[1];
+                        }
+                    }
+                    uint32_t pa[4];
+#pragma unroll
+                    for (int nb = 0; nb < 2; ++nb) {
+                        float e[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) e[i] = ex2(fmaf(s[nb][i], p.scale_log2e, -m[i >> 1]));
+                        l[0] += e[0] + e[1];
+                        l[1] += e[2] + e[3];
+                        pa[nb * 2] = pack_bf16(e[0], e[1]);
+                        pa[nb * 2 + 1] = pack_bf16(e[2], e[3]);
+                    }
                     // keys 16 kb + {2t, 2t+1} and {2t+8, 2t+9}; channels g * DH/8 ..
                     uint32_t lo[2][2], hi[2][2];          // [key pair][word]: even and odd channels of the pair's two keys
                     uint32_t s2[2];
@@ -388,8 +406,8 @@ cache4_few_kernel(const FewParams p)
                         decode8(hi[1][w], sb, yb);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            mma16816(acc[8 * w + 2 * i], pa[kb][0], pa[kb][1], pa[kb][2], pa[kb][3], xa[i], xb[i]);
-                            mma16816(acc[8 * w + 2 * i + 1], pa[kb][0], pa[kb][1], pa[kb][2], pa[kb][3], ya[i], yb[i]);
+                            mma16816(acc[8 * w + 2 * i], pa[0], pa[1], pa[2], pa[3], xa[i], xb[i]);
+                            mma16816(acc[8 * w + 2 * i + 1], pa[0], pa[1], pa[2], pa[3], ya[i], yb[i]);
                         }
                     }
                 }
@@ -398,6 +416,7 @@ cache4_few_kernel(const FewParams p)
             if (++slot == L::kDepth) slot = 0;
             at.next(p, tile + 1 < end);
         }
+        if (piece_end == row0 + 1) continue;                  // this CTA's range ends with the unit's empty tile
         // ---- the warps' results become the CTA's
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -413,8 +432,10 @@ cache4_few_kernel(const FewParams p)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             m_all[h] = -1e30f;
+#pragma unroll 1
             for (int w = 0; w < kWarps; ++w) m_all[h] = fmaxf(m_all[h], stat[(w * kFewRows + g + 8 * h) * 2]);
             l_all[h] = 0.f;
+#pragma unroll 1
             for (int w = 0; w < kWarps; ++w)
                 l_all[h] = fmaf(stat[(w * kFewRows + g + 8 * h) * 2 + 1], ex2(stat[(w * kFewRows + g + 8 * h) * 2] - m_all[h]), l_all[h]);
             const float f = ex2(m[h] - m_all[h]);
@@ -423,6 +444,7 @@ cache4_few_kernel(const FewParams p)
         }
         // a tree over the warps: n -> ceil(n / 2), the upper ones hand over through shared memory
         float4* red = (float4*)smem;
+#pragma unroll 1
         for (int n = kWarps; n > 1;) {
             const int half = (n + 1) / 2;
             if (warp >= half && warp < n)
@@ -438,14 +460,14 @@ cache4_few_kernel(const FewParams p)
             __syncthreads();
             n = half;
         }
-        const bool shared_unit = row0 < first || row0 + T > end;
+        const bool shared_unit = row0 + 1 < first || row0 + T > end;
         if (!shared_unit) {
             if (warp == 0)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = g + 8 * h;
                     if (r < rows && row_base + r < p.M) {
-                        const float inv = len > 0 ? 1.f / l_all[h] : 0.f;
+                        const float inv = 1.f / l_all[h];
                         uint4* dst = (uint4*)(p.o + (long)(row_base + r) * p.C + head * DH + t * (DH / 4));
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
@@ -455,13 +477,13 @@ cache4_few_kernel(const FewParams p)
                                     pack_bf16(acc[j][2 * h + e] * inv, acc[j + 1][2 * h + e] * inv), pack_bf16(acc[j + 2][2 * h + e] * inv, acc[j + 3][2 * h + e] * inv),
                                     pack_bf16(acc[j + 4][2 * h + e] * inv, acc[j + 5][2 * h + e] * inv), pack_bf16(acc[j + 6][2 * h + e] * inv, acc[j + 7][2 * h + e] * inv));
                         if (p.lse && t == 0)
-                            p.lse[(long)head * p.M + row_base + r] = len > 0 ? (m_all[h] + log2f(l_all[h])) * 0.69314718055994531f : -INFINITY;
+                            p.lse[(long)head * p.M + row_base + r] = (m_all[h] + log2f(l_all[h])) * 0.69314718055994531f;
                     }
                 }
             continue;
         }
         // ---- shared with other CTAs: leave the partial result, the last of them merges
-        const int c0 = cta_of(row0), c1 = cta_of(row0 + T - 1);
+        const int c0 = cta_of(row0 + 1), c1 = cta_of(row0 + T - 1);
         float* mine = p.part + ((long)blockIdx.x * 2 + ((int)blockIdx.x == c0 ? 1 : 0)) * L::kSlotFloats;
         if (warp == 0) {
 #pragma unroll
@@ -538,7 +560,7 @@ nova_status launch_few(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream
     p.tickets = ctx->dev_status + NOVA_TICKET_WORD0;
     // an upper bound of the tiles: the counts per image live on the device
     const long units = (((long)a.M + (long)c.B * (kFewRows - 1)) / kFewRows) * c.n_heads;
-    const long tiles = units * (c.Lmax / L::kTile + 1);
+    const long tiles = units * (c.Lmax / L::kTile + 2);
     const int ctas = (int)min(min((long)ctx->num_sms, (long)NOVA_TICKETS), tiles);
     static_assert(L::kTotal <= 227 * 1024, "shared memory");
     if (!ctx->attr_few) {
