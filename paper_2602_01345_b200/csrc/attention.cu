@@ -64,22 +64,26 @@ constexpr float kHugeSum = 1.2089258e24f;   // 2^80
 // waited for the epilogue of the pass before that tile's: passes up to i - kBufs - 3 are done with their slots.
 constexpr int kSlots = kBufs + 3;
 
-template <int DH, bool Q4>
+// PAIR: CTA pairs at head size 128
+template <int DH, bool Q4, bool PAIR>
 struct AttnCfg {
     static constexpr int kThreads = Q4 ? kThreads4 : kThreads512;
-    static constexpr bool kPair = (DH == 128);
+    static constexpr bool kPair = DH == 128 && PAIR;
+    static constexpr int kQBufs = DH == 128 && !PAIR ? 1 : 2;
     static constexpr int kCtas = kPair ? 2 : 1;
     static constexpr int kRows = kCtas * BQ;                    // query rows of one work item
     static constexpr int kKRows = BKV / kCtas;                  // rows of K per CTA (all of dh)
     static constexpr int kVCols = DH / kCtas;                   // columns of V per CTA (all keys)
     static constexpr int kQBytes = BQ * DH * 2;
     static constexpr int kTileBytes = kKRows * DH * 2;          // K and V alike (BKV * kVCols * 2)
-    static constexpr int kStages = Q4 ? 3 : kPair ? 4 : 5;      // stage: K of a tile and V of the tile kBufs before it
-    static constexpr int kStageOff = 2 * kQBytes;
-    // Q4: a ring of packed tiles: codes of K [kKRows][DH / 2 bytes], of V [128][32 bytes] (as tensor maps exchange their 16-byte
-    // pieces), scales of K and V [128 threads] x 4 bytes
-    static constexpr int kRing = Q4 ? 5 : 0;
-    static constexpr int kRingBytes = 4096 + 4096 + 512 + 512;
+    static constexpr int kStages = Q4 ? (DH == 128 && !PAIR ? 2 : 3) : kPair ? 4 : 5;      // stage: K of a tile and V of the tile kBufs before it
+    static constexpr int kStageOff = kQBufs * kQBytes;
+    // Q4: a ring of packed tiles: codes of K [kKRows][DH / 2 bytes] and of V [128][kVCols / 2 bytes] (as tensor maps exchange their
+    // 16-byte pieces), their scales [kKRows][DH / 64] and [128][kVCols / 64] x 4 bytes
+    static constexpr int kRing = !Q4 ? 0 : DH == 128 && !PAIR ? 2 : 5;
+    static constexpr int kCodeBytes = kKRows * DH / 2, kScaleBytes = kKRows * (DH / 64) * 4;      // K and V alike
+    static constexpr int kRingBytes = 2 * (kCodeBytes + kScaleBytes);
+    static constexpr int kUnits = kVCols / 64;                          // 64 channels of a row: how many a decoding thread has, of K and of V each
     static constexpr int kRingOff = kStageOff + kStages * 2 * kTileBytes;
     static constexpr int kLOff = kRingOff + kRing * kRingBytes;         // [kSlots][2][128] row sums of the two warpgroups
     static constexpr int kMOff = kLOff + kSlots * 2 * BQ * 4;           // [kSlots][128] reference maxima
@@ -88,8 +92,7 @@ struct AttnCfg {
     static constexpr int kBarOff = kTabOff + 64 * 52;
     static constexpr int kTotal = kBarOff + 512 + 1024;
     static_assert(kTotal <= 227 * 1024, "shared memory");
-    static_assert(kKRows * (DH / 64) == 128 && 128 * (kVCols / 64) == 128, "a decoding thread has 64 channels of a key and of a value");
-    static_assert(kVCols == 64, "a V stage is one 128-byte-wide slab");
+    static_assert(kKRows * (DH / 64) == 128 * kUnits && BKV * kVCols == kKRows * DH && kRingBytes % 1024 == 0, "K and V tiles of one size");
 };
 
 struct AttnParams {
@@ -251,10 +254,11 @@ struct Pass {
 // cu, len: cu_keep and kv_len, or copies of them in shared memory.
 // Q4: the last round's items are divided into as many parts as there are slots for, of kPartTiles tiles at least.
 constexpr int kPartTiles = 6;
-template <int DH, bool Q4>
+constexpr long kAlonePerImage = 128;      // rows per image, on average, up to which a cache in 4 bits is read by CTAs alone
+template <int DH, bool Q4, bool PAIR>
 __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu, const int32_t* len, int entry)
 {
-    constexpr int kRows = AttnCfg<DH, Q4>::kRows;
+    constexpr int kRows = AttnCfg<DH, Q4, PAIR>::kRows;
     Pass r;
     r.parts = 1;
     r.n = 0;
@@ -322,10 +326,10 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
 
 // Q4: the parts of split items become their output rows, added in the order of the parts: a row and eight columns per thread. (By the
 // epilogue's warpgroup alone, a row per thread, it took 30 us.)
-template <int DH>
+template <int DH, bool PAIR>
 __device__ __noinline__ void merge_parts(const AttnParams& p, const Pass* table, unsigned long long passes, int rank)
 {
-    constexpr int kRows = AttnCfg<DH, true>::kRows;
+    constexpr int kRows = AttnCfg<DH, true, PAIR>::kRows;
     constexpr long kPart = (long)(DH + 4) * kRows;
     const float c = p.scale_log2e;
     __threadfence();
@@ -357,14 +361,14 @@ __device__ __noinline__ void merge_parts(const AttnParams& p, const Pass* table,
     }
 }
 
-template <int DH, bool Q4>
-__global__ void __launch_bounds__(AttnCfg<DH, Q4>::kThreads, 1)
+template <int DH, bool Q4, bool PAIR>
+__global__ void __launch_bounds__(AttnCfg<DH, Q4, PAIR>::kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                  const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ AttnParams p)
 {
-    using L = AttnCfg<DH, Q4>;
+    using L = AttnCfg<DH, Q4, PAIR>;
     constexpr bool kPair = L::kPair;
-    constexpr int kStages = L::kStages;
+    constexpr int kStages = L::kStages, kQBufs = L::kQBufs;
     // Tensor memory: O (fp32, DH columns) at column 0, S buffer i (fp32) at 128 + 128 i; P (bf16 pairs) over the
     // first 64 columns of its S buffer.
     constexpr uint32_t kTmemCols = 512;
@@ -437,7 +441,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
             else if (threadIdx.x >= 128 && threadIdx.x < 128 + p.B) len_s[threadIdx.x - 128] = p.kv_len[threadIdx.x - 128];
         }
         __syncthreads();
-        if (threadIdx.x < kTable) table[threadIdx.x] = make_pass<DH, Q4>(p, copy ? cu_s : p.cu_keep, copy ? len_s : p.kv_len, me + (base + threadIdx.x) * stride);
+        if (threadIdx.x < kTable) table[threadIdx.x] = make_pass<DH, Q4, PAIR>(p, copy ? cu_s : p.cu_keep, copy ? len_s : p.kv_len, me + (base + threadIdx.x) * stride);
         if (threadIdx.x == 0) redo_s = 0;
         __syncthreads();
     };
@@ -474,7 +478,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         if constexpr (Q4) {
             const unsigned long long merges = *(volatile unsigned long long*)&merge_s;
             if (merges) {
-                if (!*abort_flag) merge_parts<DH>(p, table, merges, (int)rank);
+                if (!*abort_flag) merge_parts<DH, PAIR>(p, table, merges, (int)rank);
                 __syncthreads();
                 if (threadIdx.x == 0) merge_s = 0;
             }
@@ -526,7 +530,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             // Q alone: the last two warpgroups bring in keys and values
                             for (int i = next_pass(0, only); i < kTable && ok; i = next_pass(i + 1, only))
                                 for (int pass = only ? 0 : 1; pass < 2 && ok; ++pass) {
-                                    if (qcount >= 2 && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; break; }
+                                    if (qcount >= kQBufs && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; break; }
                                     if (rank == 0) mbar_arrive_expect_tx(&q_full[qb], L::kCtas * L::kQBytes);
 #pragma unroll
                                     for (int sl = 0; sl < DH / 64; ++sl) {
@@ -536,7 +540,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                                         else tma_load_2d(dst, &tmap_q, &q_full[qb], table[i].x + sl * 64, row);
                                     }
                                     ++qcount;
-                                    if (++qb == 2) { qb = 0; qpar ^= 1u; }
+                                    if (++qb == kQBufs) { qb = 0; qpar ^= 1u; }
                                 }
                         }
                         // one stage: V of tile vj of pass vi (vi < 0: none) and K of the next S tile, if there is one
@@ -547,7 +551,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             if (units >= kStages && !mbar_wait(&kv_empty[st], spar ^ 1u, abort_flag, p.status)) { ok = false; return; }
                             const bool has_k = s_left > 0;
                             if (has_k && s_left == s_n) {
-                                if (qcount >= 2 && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; return; }
+                                if (qcount >= kQBufs && !mbar_wait(&q_empty[qb], qpar ^ 1u, abort_flag, p.status)) { ok = false; return; }
                                 if (rank == 0) mbar_arrive_expect_tx(&q_full[qb], L::kCtas * L::kQBytes);
 #pragma unroll
                                 for (int sl = 0; sl < DH / 64; ++sl) {
@@ -557,7 +561,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                                     else tma_load_2d(dst, &tmap_q, &q_full[qb], table[si].x + sl * 64, row);
                                 }
                                 ++qcount;
-                                if (++qb == 2) { qb = 0; qpar ^= 1u; }
+                                if (++qb == kQBufs) { qb = 0; qpar ^= 1u; }
                             }
                             uint8_t* dst = smem + L::kStageOff + st * 2 * L::kTileBytes;
                             if (rank == 0)
@@ -590,11 +594,11 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         // A round ends with every copy landed and every use of a stage or of Q done.
                         for (int i = max(0, units - kStages); i < units && ok; ++i)
                             ok = mbar_wait(&kv_empty[i % kStages], (uint32_t)(i / kStages) & 1u, abort_flag, p.status);
-                        for (int i = max(0, qcount - 2); i < qcount && ok; ++i)
-                            ok = mbar_wait(&q_empty[i & 1], (uint32_t)(i >> 1) & 1u, abort_flag, p.status);
+                        for (int i = max(0, qcount - kQBufs); i < qcount && ok; ++i)
+                            ok = mbar_wait(&q_empty[i % kQBufs], (uint32_t)(i / kQBufs) & 1u, abort_flag, p.status);
                         if (!ok || *abort_flag) {       // what is in flight gets some time to finish before memory is released
                             if (rank == 0) {
-                                for (int i = max(0, qcount - 2); i < qcount; ++i) mbar_drain(&q_full[i & 1], (uint32_t)(i >> 1) & 1u);
+                                for (int i = max(0, qcount - kQBufs); i < qcount; ++i) mbar_drain(&q_full[i % kQBufs], (uint32_t)(i / kQBufs) & 1u);
                                 for (int i = max(0, units - kStages); i < units; ++i) mbar_drain(&kv_full[i % kStages], (uint32_t)(i / kStages) & 1u);
                             }
                             for (int i = max(0, units - kStages); i < units; ++i) mbar_drain(&kv_empty[i % kStages], (uint32_t)(i / kStages) & 1u);
@@ -632,7 +636,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             new_q = s_step();
                             if (new_q) {
                                 commit(&q_empty[qb]);
-                                if (++qb == 2) { qb = 0; qpar ^= 1u; }
+                                if (++qb == kQBufs) { qb = 0; qpar ^= 1u; }
                             }
                         };
                         auto take_stage = [&]() -> int {
@@ -738,27 +742,24 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         if (units >= L::kRing) ok = mbar_wait_warp(&r_empty[rs], rpar ^ 1u, abort_flag, p.status);
                         if (!ok) break;
                         uint8_t* const to = smem + L::kRingOff + rs * L::kRingBytes;
-                        const uint32_t to_s = smem_u32(to) + 8192u;
+                        const uint32_t to_k = smem_u32(to) + 2 * L::kCodeBytes, to_v = to_k + L::kScaleBytes;      // the scales
                         const int yk = (s_left == 1 ? k_last : k_y) + (int)rank * L::kKRows;
                         if (warp == 2 && elect_one()) {
                             ring_s[rs] = over ? -1 - stages : (has_k ? 1 : 0) | (has_v ? 2 : 0);
-                            mbar_arrive_expect_tx(&r_full[rs], (has_k ? 4096 : 0) + (has_v ? 4096 : 0));
+                            mbar_arrive_expect_tx(&r_full[rs], (has_k ? L::kCodeBytes : 0) + (has_v ? L::kCodeBytes : 0));
                             // (rows before the first read as zeros)
                             if (has_k) tma_load_3d(to, &tmap_k, &r_full[rs], k_x, yk, k_b);
-                            if (has_v) tma_load_3d(to + 4096, &tmap_v, &r_full[rs], xv, yv, bv);
+                            if (has_v) tma_load_3d(to + L::kCodeBytes, &tmap_v, &r_full[rs], xv, yv, bv);
                         }
                         __syncwarp();
-                        if (has_k) {
-                            if constexpr (DH == 128) copy_scales(to_s + lt * 8, k_sc, yk, lt, std::integral_constant<int, 8>());
-                            else {
-                                copy_scales(to_s + lt * 4, k_sc, yk, lt, std::integral_constant<int, 4>());
-                                copy_scales(to_s + lt * 4 + 256, k_sc + 64 * scale_row, yk, lt + 64, std::integral_constant<int, 4>());
-                            }
-                        }
-                        if (has_v) {
-                            copy_scales(to_s + 512 + lt * 4, sv, yv, lt, std::integral_constant<int, 4>());
-                            copy_scales(to_s + 768 + lt * 4, sv + 64 * scale_row, yv, lt + 64, std::integral_constant<int, 4>());
-                        }
+                        // 64 rows at a time: 4 bytes for 64 channels
+                        auto copy_rows = [&](uint32_t dst, const uint8_t* row0, int y, auto rows, auto bytes) {
+#pragma unroll
+                            for (int r = 0; r < decltype(rows)::value; r += 64)
+                                copy_scales(dst + (lt + r) * decltype(bytes)::value, row0 + r * scale_row, y, lt + r, bytes);
+                        };
+                        if (has_k) copy_rows(to_k, k_sc, yk, std::integral_constant<int, L::kKRows>(), std::integral_constant<int, DH / 16>());
+                        if (has_v) copy_rows(to_v, sv, yv, std::integral_constant<int, BKV>(), std::integral_constant<int, L::kVCols / 16>());
                         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[rs])) : "memory");
                         if (has_k) {
                             k_y += BKV;
@@ -1115,17 +1116,18 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         // (3277 rows x 29414 keys, us: one warpgroup for all 1184; one for keys and one for values, whose waits and hand-overs are then
         // paid by each stage, 904.)
         const int dt = threadIdx.x & 127;
+        // its row of K and first 64 channels; with two units per thread it has both halves of a row
         const int k_row = dt % L::kKRows, k_slab = dt / L::kKRows;
         uint8_t* const k_to = smem + L::kStageOff + k_slab * L::kKRows * 128 + k_row * 128;
         uint8_t* const v_to = smem + L::kStageOff + L::kTileBytes + dt * 128;
         // the exchange of 16-byte pieces in the ring: of rows of 64 bytes by (row / 2) mod 4, of 32 bytes by (row / 4) mod 2
-        const int k_at = DH == 128 ? k_row * 64 : k_row * 32, k_swap = DH == 128 ? k_row >> 1 & 3 : k_row >> 2 & 1;
-        const int v_at = 4096 + dt * 32, v_swap = dt >> 2 & 1;
+        const int k_at = k_row * (DH / 2), k_swap = DH == 128 ? k_row >> 1 & 3 : k_row >> 2 & 1;
+        const int v_at = L::kCodeBytes + dt * (L::kVCols / 2), v_swap = L::kVCols == 128 ? dt >> 1 & 3 : dt >> 2 & 1;
         const int turn = (warp - 16) >> 2;
         int rs = turn, st = turn, n = turn;                // ring entry, stage, stages so far; every other one
         uint32_t rpar = 0, spar = 1;                       // phases of the two
         auto next_ring = [&]() { if ((rs += 2) >= L::kRing) { rs -= L::kRing; rpar ^= 1u; } };
-        static_assert(kStages == 3 && kBufs <= kStages, "a turn of two stages passes the last one at most once");
+        static_assert(kStages >= 2 && L::kRing >= 2, "a turn of two passes the last one at most once");
         for (int base = 0; begin_round(base); base += kTable) {
             unsigned long long only = 0;
             do {
@@ -1136,14 +1138,19 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                     if (!ok) break;
                     const uint8_t* from = smem + L::kRingOff + rs * L::kRingBytes;
                     const int what = *(volatile int*)&ring_s[rs];
-                    uint4 kw[2], vw[2];
+                    constexpr int U = L::kUnits;
+                    uint4 kw[2 * U], vw[2 * U];
+                    uint32_t ksc[U], vsc[U];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        kw[h] = *(const uint4*)(from + k_at + (((DH == 128 ? k_slab * 2 : 0) + h) ^ k_swap) * 16);
+                    for (int h = 0; h < 2 * U; ++h) {
+                        kw[h] = *(const uint4*)(from + k_at + ((k_slab * 2 + h) ^ k_swap) * 16);
                         vw[h] = *(const uint4*)(from + v_at + (h ^ v_swap) * 16);
                     }
-                    const uint32_t ksc = *(const uint32_t*)(from + 8192 + (DH == 128 ? k_row * 8 + k_slab * 4 : dt * 4));
-                    const uint32_t vsc = *(const uint32_t*)(from + 8704 + dt * 4);
+#pragma unroll
+                    for (int h = 0; h < U; ++h) {
+                        ksc[h] = *(const uint32_t*)(from + 2 * L::kCodeBytes + k_row * (DH / 16) + (k_slab + h) * 4);
+                        vsc[h] = *(const uint32_t*)(from + 2 * L::kCodeBytes + L::kScaleBytes + dt * (L::kVCols / 16) + h * 4);
+                    }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&r_empty[rs]);
                     next_ring();
@@ -1164,8 +1171,11 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             *(uint4*)(dst + ((i ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
                         }
                     };
-                    if (what & 1) put(k_to, k_row, kw[0], kw[1], ksc);
-                    if (what & 2) put(v_to, dt, vw[0], vw[1], vsc);
+#pragma unroll
+                    for (int h = 0; h < U; ++h) {
+                        if (what & 1) put(k_to + h * L::kKRows * 128, k_row, kw[2 * h], kw[2 * h + 1], ksc[h]);
+                        if (what & 2) put(v_to + h * kSlabBytes, dt, vw[2 * h], vw[2 * h + 1], vsc[h]);
+                    }
                     fence_proxy_async_smem();
                     __syncwarp();
                     // (the fence hands the stage to the tensor core; a release at cluster scope would wait for much more: 1095 -> 904 us)
@@ -1196,7 +1206,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
 template <int DH>
 nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
 {
-    using L = AttnCfg<DH, false>;
+    using L = AttnCfg<DH, false, true>;
     CUtensorMap tq, tk, tv;
     const uint64_t dq[2] = {(uint64_t)a.C, (uint64_t)a.M}, sq[1] = {(uint64_t)a.C * 2};
     const uint64_t dk[3] = {(uint64_t)a.C, (uint64_t)a.Lmax, (uint64_t)a.B};
@@ -1205,8 +1215,8 @@ nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
         !make_tmap_bf16(ctx, &tv, a.v_cache, 3, dk, sk, BKV))
         return nova_fail(ctx, NOVA_ERR_CUDA, "attention: cuTensorMapEncodeTiled failed");
     if (!ctx->attr_attn) {   // both head sizes once per context
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, false>::kTotal));
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, false>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, false, true>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, false, true>::kTotal));
         ctx->attr_attn = true;
     }
     AttnParams p;
@@ -1229,7 +1239,7 @@ nova_status launch(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)
     const int ctas = (int)min((long)p.slots, (can_split ? 2 : 1) * items) * L::kCtas;
     {
         nova_launch_scope scope(ctx, NOVA_K_ATTENTION, st);
-        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, false>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
+        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, false, true>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
     }
     return NOVA_OK;
 }
@@ -1246,19 +1256,20 @@ bool make_tmap_codes(nova_ctx* ctx, CUtensorMap* map, const void* base, const no
                                                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DH>
+template <int DH, bool PAIR>
 nova_status launch4(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
 {
-    using L = AttnCfg<DH, true>;
+    using L = AttnCfg<DH, true, PAIR>;
     const nova_cache4& c = *a.cache;
     CUtensorMap tq, tk, tv;
     const uint64_t dq[2] = {(uint64_t)c.C, (uint64_t)a.M}, sq[1] = {(uint64_t)a.ldq * 2};
     if (!make_tmap_bf16(ctx, &tq, a.q, 2, dq, sq, BQ) || !make_tmap_codes(ctx, &tk, c.k_codes, c, DH / 2, L::kKRows) ||
         !make_tmap_codes(ctx, &tv, c.v_codes, c, L::kVCols / 2, BKV))
         return nova_fail(ctx, NOVA_ERR_CUDA, "cache4 attention: cuTensorMapEncodeTiled failed");
-    if (!ctx->attr_attn4) {   // both head sizes once per context
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, true>::kTotal));
-        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, true>::kTotal));
+    if (!ctx->attr_attn4) {   // all forms once per context
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<64, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<64, true, true>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, true, true>::kTotal));
+        NOVA_CUDA_CHECK(ctx, cudaFuncSetAttribute(attention_kernel<128, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<128, true, false>::kTotal));
         ctx->attr_attn4 = true;
     }
     AttnParams p;
@@ -1282,7 +1293,7 @@ nova_status launch4(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t 
     const int ctas = (int)min((long)p.slots, most) * L::kCtas;
     {
         nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
-        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, true>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
+        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(attention_kernel<DH, true, PAIR>, dim3(ctas), dim3(L::kThreads), L::kTotal, st, L::kPair ? 2 : 0, tq, tk, tv, p));
     }
     return NOVA_OK;
 }
@@ -1296,7 +1307,10 @@ size_t nova_cache4_tiles_scratch(int num_sms, int dh)
 }
 nova_status nova_launch_cache4_tiles(nova_ctx* ctx, const nova_cache4_attn_args& a, cudaStream_t st)
 {
-    return a.cache->C / a.cache->n_heads == 64 ? launch4<64>(ctx, a, st) : launch4<128>(ctx, a, st);
+    if (a.cache->C / a.cache->n_heads == 64) return launch4<64, true>(ctx, a, st);
+    // A pair's 256 rows would be half empty: CTAs alone, each with whole tiles. (Both bring in and decode as much per SM.)
+    if ((long)a.M <= kAlonePerImage * (long)a.cache->B) return launch4<128, false>(ctx, a, st);
+    return launch4<128, true>(ctx, a, st);
 }
 
 nova_status nova_launch_attention(nova_ctx* ctx, const nova_attn_args& a, cudaStream_t st)

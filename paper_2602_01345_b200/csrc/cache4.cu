@@ -5,8 +5,10 @@ namespace {
 
 using namespace c4;
 
+constexpr int kPer = 2;                // words of a row, keys and values, per thread of append and read: all loads before the first store
+
 // ---- append ------------------------------------------------------------------------------------------------
-// One thread per eight channels of a row, keys and values: 16 bytes of each in, a word of codes of each out, the four threads of
+// Per word of a row, eight channels of keys and values: 16 bytes of each in, a word of codes of each out, the four threads of
 // a group agree on its scale by two shuffles. Magnitudes are compared as integers, which orders NaN above everything.
 struct AppendParams {
     const uint4 *k, *v;
@@ -38,13 +40,15 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& x, uint16_t& scale)
     s = top ? fmaxf(s, 7.52316385e-37f) : 0.f;          // 2^-120
     scale = (uint16_t)(__float_as_uint(s) >> 16);
     if (top == 0) return 0x88888888u;
+    // x / s without a division: x times the rounded reciprocal is off by at most 2^-20, while x / s is a whole number of halves
+    // or at least 2^-10 from one. Rounded to a multiple of 2^-11 (the multiply-add's sum has no finer bits), a half comes out as
+    // exactly that, and everything else stays on its side of it; the second sum rounds to a whole number, ties to even, in the low bits.
+    const float inv = __frcp_rn(s);
+    auto code = [&](float x) { return __float_as_uint(__fadd_rn(__fadd_rn(__fmaf_rn(x, inv, 6144.f), -6144.f), 12582920.f)) & 15u; };      // 1.5 2^23 + 8
     uint32_t out = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int lo = __float2int_rn(__fdiv_rn(__uint_as_float(w[i] << 16), s));
-        const int hi = __float2int_rn(__fdiv_rn(__uint_as_float(w[i] & 0xffff0000u), s));
-        out |= (uint32_t)(lo + 8) << (4 * i) | (uint32_t)(hi + 8) << (16 + 4 * i);
-    }
+    for (int i = 0; i < 4; ++i)
+        out |= code(__uint_as_float(w[i] << 16)) << (4 * i) | code(__uint_as_float(w[i] & 0xffff0000u)) << (16 + 4 * i);
     return out;
 }
 
@@ -53,31 +57,39 @@ cache4_append_kernel(const AppendParams p)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const int vec = p.C >> 3;                            // a multiple of 8: the four threads of a group are in one warp
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    const unsigned vec = p.C >> 3;                       // a multiple of 8: the four threads of a group are in one warp
     const int rows = min(p.M, p.cu[p.B]);
-    const int r = (int)(i / vec), c = (int)(i - (long)r * vec);
-    const bool live = r < rows;
-    uint4 k = make_uint4(0, 0, 0, 0), v = k;
-    long dst = -1;
-    if (live) {
-        k = p.k[r * p.ld + c];
-        v = p.v[r * p.ld + c];
-        const int b = image_of(p.cu, p.B, r);
-        const int c0 = p.cu[b], len = p.kv_len[b];
-        if (len >= 0 && r >= c0 && (long)len + (p.cu[b + 1] - c0) <= p.Lmax) dst = (long)b * p.Lmax + len + (r - c0);
-        else atomicOr(p.status, NOVA_DEV_SHAPE);
+    uint4 k[kPer], v[kPer];
+    long dst[kPer];
+    unsigned c[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const unsigned i = blockIdx.x * (256u * kPer) + j * 256u + threadIdx.x, r = i / vec;
+        c[j] = i - r * vec;
+        dst[j] = -1;
+        k[j] = v[j] = make_uint4(0, 0, 0, 0);
+        if (r < (unsigned)rows) {
+            k[j] = p.k[r * p.ld + c[j]];
+            v[j] = p.v[r * p.ld + c[j]];
+            const int b = image_of(p.cu, p.B, (int)r);
+            const int c0 = p.cu[b], len = p.kv_len[b];
+            if (len >= 0 && (int)r >= c0 && (long)len + (p.cu[b + 1] - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
+            else atomicOr(p.status, NOVA_DEV_SHAPE);
+        }
     }
-    uint16_t ks, vs;
-    const uint32_t kc = quantise8(k, ks), vc = quantise8(v, vs);
-    if (dst >= 0) {
-        p.k_codes[dst * vec + c] = kc;
-        p.v_codes[dst * vec + c] = vc;
-        if ((c & 3) == 0) {
-            const long g = dst * (vec >> 2) + (c >> 2);
-            p.k_scales[g] = ks;
-            p.v_scales[g] = vs;
-            if (ks == 0x7fc0u || vs == 0x7fc0u) atomicOr(p.status, NOVA_DEV_NONFINITE);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        uint16_t ks, vs;
+        const uint32_t kc = quantise8(k[j], ks), vc = quantise8(v[j], vs);
+        if (dst[j] >= 0) {
+            p.k_codes[dst[j] * vec + c[j]] = kc;
+            p.v_codes[dst[j] * vec + c[j]] = vc;
+            if ((c[j] & 3) == 0) {
+                const long g = dst[j] * (vec >> 2) + (c[j] >> 2);
+                p.k_scales[g] = ks;
+                p.v_scales[g] = vs;
+                if (ks == 0x7fc0u || vs == 0x7fc0u) atomicOr(p.status, NOVA_DEV_NONFINITE);
+            }
         }
     }
     if (p.advance) {
@@ -95,7 +107,7 @@ cache4_append_kernel(const AppendParams p)
 }
 
 // ---- read ---------------------------------------------------------------------------------------------------
-// One thread per word of a row, keys and values: 4 bytes of codes in, 16 bytes out. Bound by the bytes written.
+// Per word of a row, keys and values: 4 bytes of codes in, 16 bytes out. Bound by the bytes written.
 struct ReadParams {
     const uint32_t *k_codes, *v_codes;
     const uint16_t *k_scales, *v_scales;
@@ -111,25 +123,39 @@ cache4_read_kernel(const ReadParams p)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const int vec = p.C >> 3;
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    const int r = (int)(i / vec), c = (int)(i - (long)r * vec);
-    if (r >= min(p.M, p.cu[p.B])) return;
-    const int b = image_of(p.cu, p.B, r);
-    const long row = (long)(p.first ? p.first[b] : 0) + (r - p.cu[b]);
-    if (row < 0 || row >= p.Lmax) {
-        atomicOr(p.status, NOVA_DEV_SHAPE);
-        return;
+    const unsigned vec = p.C >> 3;
+    const int rows = min(p.M, p.cu[p.B]);
+    uint32_t kw[kPer], vw[kPer];
+    uint16_t ks[kPer], vs[kPer];
+    long to[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const unsigned i = blockIdx.x * (256u * kPer) + j * 256u + threadIdx.x, r = i / vec, c = i - r * vec;
+        to[j] = -1;
+        if (r < (unsigned)rows) {
+            const int b = image_of(p.cu, p.B, (int)r);
+            const long row = (long)(p.first ? p.first[b] : 0) + ((int)r - p.cu[b]);
+            if (row >= 0 && row < p.Lmax) {
+                const long src = (long)b * p.Lmax + row, g = src * (vec >> 2) + (c >> 2);
+                to[j] = r * p.ld + c;
+                kw[j] = p.k_codes[src * vec + c];
+                vw[j] = p.v_codes[src * vec + c];
+                ks[j] = p.k_scales[g];
+                vs[j] = p.v_scales[g];
+            } else {
+                atomicOr(p.status, NOVA_DEV_SHAPE);
+            }
+        }
     }
-    const long src = (long)b * p.Lmax + row;
-    const uint32_t kw = p.k_codes[src * vec + c], vw = p.v_codes[src * vec + c];
-    const long g = src * (vec >> 2) + (c >> 2);
-    const Scale2 ks(both(p.k_scales[g])), vs(both(p.v_scales[g]));
-    uint32_t x[4];
-    decode8(kw, ks, x);
-    p.k[r * p.ld + c] = make_uint4(x[0], x[1], x[2], x[3]);
-    decode8(vw, vs, x);
-    p.v[r * p.ld + c] = make_uint4(x[0], x[1], x[2], x[3]);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (to[j] >= 0) {
+            uint32_t x[4];
+            decode8(kw[j], Scale2(both(ks[j])), x);
+            __stcs(p.k + to[j], make_uint4(x[0], x[1], x[2], x[3]));
+            decode8(vw[j], Scale2(both(vs[j])), x);
+            __stcs(p.v + to[j], make_uint4(x[0], x[1], x[2], x[3]));
+        }
 }
 
 // ---- eviction: which rows stay ---------------------------------------------------------------------------------
@@ -265,7 +291,8 @@ cache4_evict_select(const EvictParams p)
 }
 
 // ---- eviction: the rows move --------------------------------------------------------------------------------------
-// One warp per row of the new cache: codes in 16-byte pieces, scales in 4-byte pieces, the weight. Bound by the bytes.
+// One warp for two rows of the new cache: codes in 16-byte pieces, scales in 4-byte pieces, the weight. Bound by the bytes.
+constexpr int kMoveRows = 2;
 struct MoveParams {
     const uint4 *k_codes, *v_codes;
     const uint32_t *k_scales, *v_scales;
@@ -283,28 +310,38 @@ cache4_move_kernel(const MoveParams p)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const int lane = threadIdx.x & 31;
-    const long r = (long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (r >= p.rows) return;
-    const int per = p.weight_out ? p.Lmax_out : p.budget;
-    const int b = (int)(r / per), i = (int)(r - (long)b * per);
-    const int s = i < p.budget ? p.src_row[(long)b * p.budget + i] : -1;
-    if ((unsigned)s >= (unsigned)p.Lmax) {
-        if (lane == 0 && p.weight_out) p.weight_out[(long)b * p.Lmax_out + i] = 0.f;
-        return;
-    }
-    const long src = (long)b * p.Lmax + s, dst = (long)b * p.Lmax_out + i;
+    const int lane = threadIdx.x & 31, per = p.weight_out ? p.Lmax_out : p.budget;
+    const long r0 = ((long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kMoveRows;
     const int pieces = p.C >> 5, words = p.C >> 6;
-    if (lane == 0 && p.weight_out) p.weight_out[dst] = p.weight[src];
+    long src[kMoveRows], dst[kMoveRows];
+#pragma unroll
+    for (int j = 0; j < kMoveRows; ++j) {
+        src[j] = -1;
+        const long r = r0 + j;
+        if (r >= p.rows) continue;
+        const int b = (int)(r / per), i = (int)(r - (long)b * per);
+        const int s = i < p.budget ? p.src_row[(long)b * p.budget + i] : -1;
+        dst[j] = (long)b * p.Lmax_out + i;
+        if ((unsigned)s < (unsigned)p.Lmax) src[j] = (long)b * p.Lmax + s;
+        if (lane == 0 && p.weight_out) p.weight_out[dst[j]] = src[j] >= 0 ? p.weight[src[j]] : 0.f;
+    }
     for (int c = lane; c < pieces; c += 32) {
-        const uint4 k = p.k_codes[src * pieces + c], v = p.v_codes[src * pieces + c];
-        p.k_codes_out[dst * pieces + c] = k;
-        p.v_codes_out[dst * pieces + c] = v;
+        uint4 k[kMoveRows], v[kMoveRows];
+#pragma unroll
+        for (int j = 0; j < kMoveRows; ++j)
+            if (src[j] >= 0) { k[j] = p.k_codes[src[j] * pieces + c]; v[j] = p.v_codes[src[j] * pieces + c]; }
+#pragma unroll
+        for (int j = 0; j < kMoveRows; ++j)
+            if (src[j] >= 0) { p.k_codes_out[dst[j] * pieces + c] = k[j]; p.v_codes_out[dst[j] * pieces + c] = v[j]; }
     }
     for (int c = lane; c < words; c += 32) {
-        const uint32_t k = p.k_scales[src * words + c], v = p.v_scales[src * words + c];
-        p.k_scales_out[dst * words + c] = k;
-        p.v_scales_out[dst * words + c] = v;
+        uint32_t k[kMoveRows], v[kMoveRows];
+#pragma unroll
+        for (int j = 0; j < kMoveRows; ++j)
+            if (src[j] >= 0) { k[j] = p.k_scales[src[j] * words + c]; v[j] = p.v_scales[src[j] * words + c]; }
+#pragma unroll
+        for (int j = 0; j < kMoveRows; ++j)
+            if (src[j] >= 0) { p.k_scales_out[dst[j] * words + c] = k[j]; p.v_scales_out[dst[j] * words + c] = v[j]; }
     }
 }
 
@@ -357,8 +394,8 @@ nova_status nova_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* 
     if (rc == NOVA_OK) rc = nova_cache4_check_rows(ctx, "nova_cache4_append", c, k, v, cu_rows, M, ld);
     if (rc != NOVA_OK) return rc;
     if (M == 0 || c->B == 0) return NOVA_OK;
-    const long blocks = ((long)M * (c->C / 8) + 255) / 256;
-    if (blocks > 0x7fffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_append: too many rows");
+    const long blocks = ((long)M * (c->C / 8) + 256 * kPer - 1) / (256 * kPer);
+    if (blocks * 256 * kPer > 0xffffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_append: too many rows");
     NOVA_DEVICE_GUARD(ctx, "nova_cache4_append");
     cudaStream_t st = (cudaStream_t)stream;
     rc = nova_debug_check_lists(ctx, "nova_cache4_append", nullptr, nullptr, cu_rows, c->B, M, M, false, st);
@@ -384,8 +421,8 @@ nova_status nova_cache4_read(nova_ctx* ctx, const nova_cache4* c, const int32_t*
     if (rc == NOVA_OK) rc = nova_cache4_check_rows(ctx, "nova_cache4_read", c, k_out, v_out, cu_rows, M, ld);
     if (rc != NOVA_OK) return rc;
     if (M == 0 || c->B == 0) return NOVA_OK;
-    const long blocks = ((long)M * (c->C / 8) + 255) / 256;
-    if (blocks > 0x7fffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_read: too many rows");
+    const long blocks = ((long)M * (c->C / 8) + 256 * kPer - 1) / (256 * kPer);
+    if (blocks * 256 * kPer > 0xffffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_read: too many rows");
     NOVA_DEVICE_GUARD(ctx, "nova_cache4_read");
     cudaStream_t st = (cudaStream_t)stream;
     rc = nova_debug_check_lists(ctx, "nova_cache4_read", nullptr, nullptr, cu_rows, c->B, M, M, false, st);
@@ -437,7 +474,7 @@ nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* 
     m.weight = weight; m.weight_out = weight_out; m.src_row = list;
     m.Lmax = c->Lmax; m.Lmax_out = dst->Lmax; m.budget = budget; m.C = c->C;
     m.rows = (long)c->B * (weight_out ? dst->Lmax : budget);
-    const long blocks = (m.rows + 7) / 8;
+    const long blocks = (m.rows + 8 * kMoveRows - 1) / (8 * kMoveRows);
     const int keys = (int)((c->Lmax + kEvThreads - 1) / kEvThreads);
     if (blocks > 0x7fffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_evict: too many rows");
     NOVA_DEVICE_GUARD(ctx, "nova_cache4_evict");

@@ -3,9 +3,9 @@
 // A row of C channels is C/8 32-bit words of codes and C/32 scales. Each group of 32 channels shares a scale
 // s: its largest magnitude over 7, rounded up to five significant bits (so no code is clipped), held as bf16. A channel is
 // a code in [-7, 7] times s. Three bits times five: every decoded value is exact in bf16, so what the tensor core multiplies
-// is the value the cache stands for. Both divisions are correctly rounded and leave no doubt: x / s of a bf16 x is either
-// exactly half way between two codes or at least 2^-10 from it, and the largest magnitude over 7 is either a number of five
-// bits or at least 2^-11 (relative) from one.
+// is the value the cache stands for. Neither rounding leaves a doubt: x / s of a bf16 x is either exactly half way between two
+// codes or at least 2^-10 from it, and the largest magnitude over 7 is either a number of five bits or at least 2^-11 (relative)
+// from one.
 // A word holds the codes plus 8 of eight channels c..c+7: channel c+2i in bits 4i..4i+3, c+2i+1 in bits 16+4i..19+4i, so that
 // one shift and one logical operation give a pair of neighbouring channels as two bf16 numbers 128 + 8 (code + 8), and one
 // fused multiply-add by s/8 and -24 s the two values: (128 + 8 u) s/8 - 24 s = (u - 8) s with all operands and the result exact.

@@ -22,7 +22,7 @@ namespace {
 using namespace c4;
 
 constexpr int kFewRows = 16;           // query rows of a unit
-constexpr long kFewPerImage = 24;      // rows per image, on average, up to which the launch takes this kernel
+constexpr long kFewPerImage = 16;      // rows per image, on average, up to which the launch takes this kernel
 constexpr int kWarpKeys = 32;          // keys of a warp's tile
 constexpr float kRescale = 8.f;        // the maximum follows when it is exceeded by more than this (log2)
 
