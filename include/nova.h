@@ -617,6 +617,22 @@ nova_status nova_cache4_weights(nova_ctx* ctx, const nova_cache4* c, const void*
 nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* weight, int budget, int recent,
                               const nova_cache4* dst, float* weight_out, int32_t* src_row, void* stream);
 
+/*
+ * nova_pruned_block_forward_ext (mod and ext may be NULL) on a cache in 4 bits: the kept rows' keys and values are rounded and
+ * written behind the cache's rows, and the queries attend to all of them as they are held (Eq. 14 with the values of the 4-bit rows).
+ * cache: B, C, n_heads and Lmax as in s. append_kv != 0 advances its kv_len. weight: NULL, or device f32 [B, Lmax] (then
+ * append_kv must not be 0): the weights that this call's queries give to the rows, its own among them, are added; entries at or past
+ * kv_len[b] must be zero before. An image whose rows do not fit in Lmax records NOVA_ERR_SHAPE as in nova_cache4_append.
+ * Workspace: nova_block_cache4_workspace_bytes. Everything else, errors included, as for the other block calls.
+ */
+size_t      nova_block_cache4_workspace_bytes(const nova_ctx* ctx, const nova_block_shape* s);
+nova_status nova_pruned_block_forward_cache4(nova_ctx* ctx, const nova_block_weights* w,
+                                             const nova_block_modulation* mod, const nova_block_extras* ext,
+                                             const nova_block_shape* s, const void* x_in,
+                                             const int32_t* keep_idx, const int32_t* cu_keep,
+                                             const nova_cache4* cache, float* weight, int append_kv,
+                                             void* y_kept, int m_on_device, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

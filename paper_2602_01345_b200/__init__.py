@@ -13,6 +13,6 @@ from .binding import (  # noqa: F401
     nova_restore_from_cache_device, nova_pruned_block_forward_adaln, MODULATION_NAMES,
     nova_pruned_layer_forward, nova_pruned_block_forward_ext, EXTRA_NAMES, nova_score_mse, nova_score_attention_mass, nova_scale_entropy_layers, nova_keep_ratios_layers, nova_select_topk_grouped, nova_keep_ratios_layers_device,
     Cache4, nova_cache4_workspace_bytes, nova_cache4_append, nova_cache4_read, nova_cache4_attention,
-    nova_cache4_weights, nova_cache4_evict,
+    nova_cache4_weights, nova_cache4_evict, nova_block_cache4_workspace_bytes, nova_pruned_block_forward_cache4,
     lib_path, STATUS_NAMES,
 )

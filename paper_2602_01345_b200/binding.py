@@ -201,6 +201,11 @@ class Context:
         if self._workspace is None or self._workspace.numel() < need:
             self.set_workspace(torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{self.device}"))
 
+    def ensure_block_cache4_workspace(self, shape: BlockShape):
+        need = nova_block_cache4_workspace_bytes(self, shape)
+        if self._workspace is None or self._workspace.numel() < need:
+            self.set_workspace(torch.empty(need + 256, dtype=torch.uint8, device=f"cuda:{self.device}"))
+
     def set_wait_limit_ns(self, ns: int):
         """Limit of every device-side wait of this context's later launches (0 = default, 1 s)."""
         _lib.nova_set_wait_limit_ns.argtypes = [_vp, C.c_ulonglong]
@@ -583,6 +588,18 @@ _lib.nova_pruned_block_forward_ext.argtypes = [_vp, C.POINTER(_BlockWeights), C.
 _lib.nova_pruned_block_forward_ext.restype = _i
 
 
+def _extras_struct(shape: BlockShape, extras, qk_eps: float):
+    """The C struct of a dict of extras (names from EXTRA_NAMES; missing or None = absent)."""
+    e = {n: (extras.get(n) if extras else None) for n in EXTRA_NAMES}
+    dh = shape.C // shape.n_heads
+    for n in ("rope_cos", "rope_sin"):
+        assert e[n] is None or (e[n].dtype == torch.float32 and e[n].shape == (shape.N, dh // 2))
+    Lc = e["cond_k"].shape[1] if e["cond_k"] is not None else 0
+    return _BlockExtras(_ptr(e["rope_cos"]), _ptr(e["rope_sin"]), _ptr(e["qk_gain_q"]), _ptr(e["qk_gain_k"]), qk_eps,
+                        *[_ptr(e[n]) for n in ("lnc_g", "lnc_b", "w_q2", "b_q2", "w_o2", "b_o2", "cond_k", "cond_v", "cond_len")],
+                        Lc)
+
+
 def nova_pruned_block_forward_ext(ctx: Context, w: BlockWeights, modulation, extras: dict, shape: BlockShape, x_in,
                                   keep_idx, cu_keep, k_cache, v_cache, kv_len, append_kv, y_kept,
                                   m_on_device: bool = False, qk_eps: float = 1e-12, stream=None):
@@ -590,14 +607,7 @@ def nova_pruned_block_forward_ext(ctx: Context, w: BlockWeights, modulation, ext
     names from EXTRA_NAMES to device tensors (missing or None = absent): rope_cos / rope_sin f32 [N, dh/2];
     qk_gain_q / qk_gain_k bf16 [C]; lnc_g, lnc_b, b_q2, b_o2 bf16 [C], w_q2, w_o2 bf16 [C, C], cond_k / cond_v
     bf16 [B, Lc_max, C], cond_len int32 [B] for the cross-attention."""
-    e = {n: (extras.get(n) if extras else None) for n in EXTRA_NAMES}
-    dh = shape.C // shape.n_heads
-    for n in ("rope_cos", "rope_sin"):
-        assert e[n] is None or (e[n].dtype == torch.float32 and e[n].shape == (shape.N, dh // 2))
-    Lc = e["cond_k"].shape[1] if e["cond_k"] is not None else 0
-    ce = _BlockExtras(_ptr(e["rope_cos"]), _ptr(e["rope_sin"]), _ptr(e["qk_gain_q"]), _ptr(e["qk_gain_k"]), qk_eps,
-                      *[_ptr(e[n]) for n in ("lnc_g", "lnc_b", "w_q2", "b_q2", "w_o2", "b_o2", "cond_k", "cond_v", "cond_len")],
-                      Lc)
+    ce = _extras_struct(shape, extras, qk_eps)
     ptrs = []
     for n in MODULATION_NAMES:
         t = modulation.get(n) if modulation else None
@@ -852,3 +862,30 @@ def nova_cache4_evict(ctx: Context, cache: Cache4, weight, budget: int, recent: 
     assert src_row is None or (src_row.dtype is torch.int32 and src_row.shape == (cache.B, budget) and src_row.is_contiguous())
     _, wp, _, op, rp = _on4(ctx, cache.kv_len, weight, dst.kv_len, weight_out, src_row)
     ctx.check(_lib.nova_cache4_evict(ctx.handle, cache.ref, wp, budget, recent, dst.ref, op, rp, _stream(stream)))
+
+
+_lib.nova_block_cache4_workspace_bytes.argtypes = [_vp, C.POINTER(_BlockShape)]
+_lib.nova_block_cache4_workspace_bytes.restype = C.c_size_t
+_lib.nova_pruned_block_forward_cache4.argtypes = [_vp, C.POINTER(_BlockWeights), C.POINTER(_BlockModulation), C.POINTER(_BlockExtras),
+                                                  C.POINTER(_BlockShape), _vp, _vp, _vp, C.POINTER(_Cache4), _vp, _i, _vp, _i, _vp]
+_lib.nova_pruned_block_forward_cache4.restype = _i
+
+
+def nova_block_cache4_workspace_bytes(ctx: Context, shape: BlockShape) -> int:
+    c = shape._c()
+    return int(_lib.nova_block_cache4_workspace_bytes(ctx.handle, C.byref(c)))
+
+
+def nova_pruned_block_forward_cache4(ctx: Context, w: BlockWeights, shape: BlockShape, x_in, keep_idx, cu_keep, cache: Cache4, append_kv,
+                                     y_kept, weight=None, modulation=None, extras=None, m_on_device: bool = False, qk_eps: float = 1e-12,
+                                     stream=None):
+    """The block on the kept rows with its keys and values in a 4-bit cache (Cache4). weight: f32 [B, Lmax] or None, to which the
+    attention weight of every cached row is added. modulation and extras as in nova_pruned_block_forward_ext. Needs a workspace
+    (Context.ensure_block_cache4_workspace)."""
+    assert weight is None or (weight.dtype == torch.float32 and weight.shape == (cache.B, cache.Lmax))
+    cm = modulation_struct(modulation, shape.B, shape.C) if modulation else None
+    ce = _extras_struct(shape, extras, qk_eps) if extras else None
+    c = shape._c()
+    ctx.check(_lib.nova_pruned_block_forward_cache4(
+        ctx.handle, C.byref(w.c), C.byref(cm) if cm is not None else None, C.byref(ce) if ce is not None else None, C.byref(c), _ptr(x_in),
+        _ptr(keep_idx), _ptr(cu_keep), cache.ref, _ptr(weight), int(bool(append_kv)), _ptr(y_kept), int(bool(m_on_device)), _stream(stream)))

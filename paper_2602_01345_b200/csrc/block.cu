@@ -2,7 +2,7 @@
 // attention, output projection + residual, LayerNorm, MLP with tanh-GELU + residual.
 // This file holds the small memory-bound kernels (row maps, LayerNorm, kv_len update), the
 // workspace layout and the launch sequence; the contractions live in gemm.cu / attention.cu.
-#include "common.cuh"
+#include "cache4.cuh"
 
 namespace {
 
@@ -15,7 +15,7 @@ namespace {
 struct RowMapArgs {
     const int32_t* keep_idx;
     const int32_t* cu_keep;
-    const int32_t* kv_len;
+    const int32_t* kv_len;   // NULL: keys and values stay compacted, kv_row[r] = r
     int B, N, Lmax;
     int32_t* src_row;
     int32_t* kv_row;
@@ -174,10 +174,12 @@ layernorm_rows(const uint4* x, const uint4* gamma, const uint4* beta, float eps,
             if (AHEAD) load(src_next, next);
         }
         if (MAPS && tid == 0) {
-            const int c0 = maps.cu_keep[img], k_b = maps.cu_keep[img + 1] - c0, len = maps.kv_len[img];
+            const int c0 = maps.cu_keep[img], k_b = maps.cu_keep[img + 1] - c0, len = maps.kv_len ? maps.kv_len[img] : 0;
             maps.src_row[r] = (int32_t)src;
             maps.img_row[r] = img;
-            if (len + k_b > maps.Lmax) {
+            if (!maps.kv_len) {
+                maps.kv_row[r] = r;
+            } else if (len + k_b > maps.Lmax) {
                 maps.kv_row[r] = -1;
                 atomicOr(maps.status, NOVA_DEV_SHAPE);
             } else {
@@ -365,14 +367,20 @@ struct Workspace {
     int32_t* kv_row;
     int32_t* img_row;
     __nv_bfloat16 *h, *q, *o, *x1, *f;
+    // with a cache in 4 bits: the kept rows' keys and values, their log-sum-exps, memory for shared work items
+    __nv_bfloat16 *k, *v;
+    float* lse;
+    void* scratch;
+    size_t scratch_bytes;
     size_t bytes;
 };
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-Workspace carve(void* base, int M, int C, int F)
+Workspace carve(void* base, int M, int C, int F, int heads4 = 0, int num_sms = 0)
 {
     Workspace w;
+    memset(&w, 0, sizeof(w));
     size_t off = 0;
     auto take = [&](size_t bytes) { void* p = base ? (char*)base + off : nullptr; off += align_up(bytes); return p; };
     const size_t Mp = (size_t)((M + 127) / 128) * 128;   // whole 128-row tiles
@@ -384,6 +392,13 @@ Workspace carve(void* base, int M, int C, int F)
     w.x1 = (__nv_bfloat16*)take(Mp * C * 2);
     w.f = (__nv_bfloat16*)take(Mp * (size_t)F * 2);
     w.img_row = (int32_t*)take(Mp * 4);
+    if (heads4 > 0) {
+        w.k = (__nv_bfloat16*)take(Mp * C * 2);
+        w.v = (__nv_bfloat16*)take(Mp * C * 2);
+        w.lse = (float*)take(Mp * (size_t)heads4 * 4);
+        w.scratch_bytes = max(nova_cache4_attention_scratch(num_sms, C / heads4, M), nova_cache4_weights_scratch(num_sms));
+        w.scratch = take(w.scratch_bytes);
+    }
     w.bytes = off;
     return w;
 }
@@ -469,7 +484,8 @@ static nova_status block_forward(nova_ctx* ctx, const nova_block_weights* w, con
                                  const int32_t* keep_idx, const int32_t* cu_keep,
                                  void* k_cache, void* v_cache, int32_t* kv_len,
                                  int append_kv, void* y_kept, void* stream, bool m_on_device,
-                                 const ScatterOut* scatter = nullptr, const nova_block_extras* ext = nullptr)
+                                 const ScatterOut* scatter = nullptr, const nova_block_extras* ext = nullptr,
+                                 const nova_cache4* c4 = nullptr, float* weight4 = nullptr)
 {
     if (!ctx) return NOVA_ERR_INVALID_ARG;
     if (!w || !s) return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_pruned_block_forward: null weights or shape");
@@ -485,7 +501,7 @@ static nova_status block_forward(nova_ctx* ctx, const nova_block_weights* w, con
     }
     if (!nova_aligned16(x_in) || !nova_aligned16(k_cache) || !nova_aligned16(v_cache) || !nova_aligned16(y_kept))
         return nova_fail(ctx, NOVA_ERR_ALIGNMENT, "nova_pruned_block_forward: tensor not 16-byte aligned");
-    Workspace ws = carve(ctx->workspace, s->M, s->C, s->F);
+    Workspace ws = carve(ctx->workspace, s->M, s->C, s->F, c4 ? s->n_heads : 0, ctx->num_sms);
     if (!ctx->workspace || ctx->workspace_bytes < ws.bytes)
         return nova_fail(ctx, NOVA_ERR_WORKSPACE, "nova_pruned_block_forward: workspace missing or too small");
     const bool rope = ext && (ext->rope_cos || ext->rope_sin);
@@ -529,11 +545,15 @@ static nova_status block_forward(nova_ctx* ctx, const nova_block_weights* w, con
     nova_status rc;
     // h = LN1(gathered rows); the same kernel writes the row maps the GEMM epilogues use
     RowMapArgs maps;
-    maps.keep_idx = keep_idx; maps.cu_keep = cu_keep; maps.kv_len = kv_len; maps.B = s->B; maps.N = s->N;
+    maps.keep_idx = keep_idx; maps.cu_keep = cu_keep; maps.kv_len = c4 ? nullptr : kv_len; maps.B = s->B; maps.N = s->N;
     maps.Lmax = s->Lmax; maps.src_row = ws.src_row; maps.kv_row = ws.kv_row; maps.img_row = ws.img_row; maps.status = ctx->dev_status;
     rc = launch_ln(ctx, (cbf)x_in, &maps, ln1_mod, (cbf)w->ln1_g, (cbf)w->ln1_b, w->eps, M, m_dev, C, ws.h, st);
     if (rc) return rc;
-    // [q | k | v] = h W_qkv^T + b; k, v go straight to their cache rows
+    // [q | k | v] = h W_qkv^T + b; k, v go straight to their cache rows (to be rounded first if the cache holds 4 bits)
+    if (c4) {
+        k_cache = ws.k;
+        v_cache = ws.v;
+    }
     nova_gemm_args g;
     memset(&g, 0, sizeof(g));
     g.A = ws.h; g.W = (cbf)w->w_qkv; g.bias = (cbf)w->b_qkv; g.M = M; g.m_dev = m_dev; g.N = 3 * C; g.K = C;
@@ -559,6 +579,20 @@ static nova_status block_forward(nova_ctx* ctx, const nova_block_weights* w, con
                                                            (cfl)ext->rope_cos, (cfl)ext->rope_sin);
         NOVA_CUDA_CHECK(ctx, qe);
     }
+    if (c4) {
+        // the kept rows behind the cache's, without advancing its lengths, which the last GEMM does; then all of them are attended to
+        rc = nova_launch_cache4_append(ctx, c4, ws.k, ws.v, C, cu_keep, M, 0, st);
+        if (rc) return rc;
+        nova_cache4_attn_args a4;
+        a4.cache = c4; a4.q = ws.q; a4.ldq = C; a4.cu = cu_keep; a4.M = M; a4.o = ws.o; a4.lse = weight4 ? ws.lse : nullptr;
+        a4.own_rows = true; a4.scratch = ws.scratch; a4.scratch_bytes = ws.scratch_bytes;
+        rc = nova_launch_cache4_attention(ctx, a4, st);
+        if (rc) return rc;
+        if (weight4) {
+            rc = nova_launch_cache4_weights(ctx, c4, ws.q, C, ws.lse, cu_keep, M, weight4, weight4, true, ws.scratch, ws.scratch_bytes, st);
+            if (rc) return rc;
+        }
+    } else {
     // o = softmax(q K^T / sqrt(dh)) V
     nova_attn_args a;
     a.q = ws.q; a.k_cache = (cbf)k_cache; a.v_cache = (cbf)v_cache; a.cu_keep = cu_keep; a.kv_len = kv_len;
@@ -570,6 +604,7 @@ static nova_status block_forward(nova_ctx* ctx, const nova_block_weights* w, con
     a.cache_only = false;
     rc = nova_launch_attention(ctx, a, st);
     if (rc) return rc;
+    }
     // x1 = Xc + o W_o^T + b_o
     memset(&g, 0, sizeof(g));
     g.A = ws.o; g.W = (cbf)w->w_o; g.bias = (cbf)w->b_o; g.M = M; g.m_dev = m_dev; g.N = C; g.K = C;
@@ -699,6 +734,31 @@ extern "C" nova_status nova_pruned_block_forward_ext(nova_ctx* ctx, const nova_b
 {
     return block_forward(ctx, w, mod, s, x_in, keep_idx, cu_keep, k_cache, v_cache, kv_len, append_kv, y_kept, stream,
                          m_on_device != 0, nullptr, ext);
+}
+
+extern "C" size_t nova_block_cache4_workspace_bytes(const nova_ctx* ctx, const nova_block_shape* s)
+{
+    if (!ctx || !shape_ok(s)) return 0;
+    return carve(nullptr, s->M, s->C, s->F, s->n_heads, ctx->num_sms).bytes;
+}
+
+extern "C" nova_status nova_pruned_block_forward_cache4(nova_ctx* ctx, const nova_block_weights* w,
+                                                        const nova_block_modulation* mod, const nova_block_extras* ext,
+                                                        const nova_block_shape* s, const void* x_in,
+                                                        const int32_t* keep_idx, const int32_t* cu_keep,
+                                                        const nova_cache4* cache, float* weight, int append_kv,
+                                                        void* y_kept, int m_on_device, void* stream)
+{
+    if (!ctx) return NOVA_ERR_INVALID_ARG;
+    const nova_status rc = nova_cache4_check(ctx, "nova_pruned_block_forward_cache4", cache);
+    if (rc != NOVA_OK) return rc;
+    if (!s || s->B != cache->B || s->C != cache->C || s->n_heads != cache->n_heads || s->Lmax != cache->Lmax)
+        return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_pruned_block_forward_cache4: shape and cache differ");
+    if (weight && !append_kv)
+        return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_pruned_block_forward_cache4: weights are kept of rows that stay (append_kv)");
+    if (((uintptr_t)weight) & 3u) return nova_fail(ctx, NOVA_ERR_ALIGNMENT, "nova_pruned_block_forward_cache4: misaligned weights");
+    return block_forward(ctx, w, mod, s, x_in, keep_idx, cu_keep, cache->k_codes, cache->v_codes, cache->kv_len, append_kv, y_kept, stream,
+                         m_on_device != 0, nullptr, ext, cache, weight);
 }
 
 // Eq. 14 followed by Eq. 15-16 for one layer: the block on the kept rows with its last GEMM writing

@@ -384,6 +384,23 @@ nova_status nova_cache4_check_rows(nova_ctx* ctx, const char* who, const nova_ca
     return NOVA_OK;
 }
 
+nova_status nova_launch_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* k, const void* v, int64_t ld, const int32_t* cu,
+                                      int M, int advance, cudaStream_t st)
+{
+    if (M == 0 || c->B == 0) return NOVA_OK;
+    const long blocks = ((long)M * (c->C / 8) + 256 * kPer - 1) / (256 * kPer);
+    if (blocks * 256 * kPer > 0xffffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_append: too many rows");
+    AppendParams p;
+    p.k = (const uint4*)k; p.v = (const uint4*)v; p.ld = ld / 8; p.cu = cu; p.kv_len = c->kv_len;
+    p.k_codes = (uint32_t*)c->k_codes; p.v_codes = (uint32_t*)c->v_codes;
+    p.k_scales = (uint16_t*)c->k_scales; p.v_scales = (uint16_t*)c->v_scales;
+    p.B = c->B; p.M = M; p.C = c->C; p.Lmax = c->Lmax; p.advance = advance != 0;
+    p.status = ctx->dev_status; p.ticket = ctx->dev_status + NOVA_APPEND_TICKET_WORD;
+    nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
+    NOVA_CUDA_CHECK(ctx, nova_launch_pdl(cache4_append_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 0, p));
+    return NOVA_OK;
+}
+
 extern "C" {
 
 nova_status nova_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* k, const void* v, int64_t ld,
@@ -394,23 +411,11 @@ nova_status nova_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* 
     if (rc == NOVA_OK) rc = nova_cache4_check_rows(ctx, "nova_cache4_append", c, k, v, cu_rows, M, ld);
     if (rc != NOVA_OK) return rc;
     if (M == 0 || c->B == 0) return NOVA_OK;
-    const long blocks = ((long)M * (c->C / 8) + 256 * kPer - 1) / (256 * kPer);
-    if (blocks * 256 * kPer > 0xffffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_append: too many rows");
     NOVA_DEVICE_GUARD(ctx, "nova_cache4_append");
     cudaStream_t st = (cudaStream_t)stream;
     rc = nova_debug_check_lists(ctx, "nova_cache4_append", nullptr, nullptr, cu_rows, c->B, M, M, false, st);
     if (rc != NOVA_OK) return rc;
-    AppendParams p;
-    p.k = (const uint4*)k; p.v = (const uint4*)v; p.ld = ld / 8; p.cu = cu_rows; p.kv_len = c->kv_len;
-    p.k_codes = (uint32_t*)c->k_codes; p.v_codes = (uint32_t*)c->v_codes;
-    p.k_scales = (uint16_t*)c->k_scales; p.v_scales = (uint16_t*)c->v_scales;
-    p.B = c->B; p.M = M; p.C = c->C; p.Lmax = c->Lmax; p.advance = advance != 0;
-    p.status = ctx->dev_status; p.ticket = ctx->dev_status + NOVA_APPEND_TICKET_WORD;
-    {
-        nova_launch_scope scope(ctx, NOVA_K_CACHE4, st);
-        NOVA_CUDA_CHECK(ctx, nova_launch_pdl(cache4_append_kernel, dim3((unsigned)blocks), dim3(256), 0, st, 0, p));
-    }
-    return NOVA_OK;
+    return nova_launch_cache4_append(ctx, c, k, v, ld, cu_rows, M, advance, st);
 }
 
 nova_status nova_cache4_read(nova_ctx* ctx, const nova_cache4* c, const int32_t* first, const int32_t* cu_rows, int M,

@@ -75,6 +75,9 @@ nova_status nova_cache4_check(nova_ctx* ctx, const char* who, const nova_cache4*
 nova_status nova_cache4_check_rows(nova_ctx* ctx, const char* who, const nova_cache4* c, const void* a, const void* b,
                                    const int32_t* cu_rows, int M, int64_t ld);
 
+nova_status nova_launch_cache4_append(nova_ctx* ctx, const nova_cache4* c, const void* k, const void* v, int64_t ld, const int32_t* cu,
+                                      int M, int advance, cudaStream_t st);
+
 // Attention over the cache. own_rows: the keys of image b are its kv_len[b] rows and the cu[b+1] - cu[b] behind them (appended
 // without advancing the lengths), else the kv_len[b] rows alone.
 struct nova_cache4_attn_args {

@@ -25,8 +25,11 @@ class PrunedScaleRunner:
 
     def __init__(self, ctx: nv.Context, weights, n_heads: int, B: int, h: int, w: int, Lmax: int,
                  k_caches, v_caches, kv_len, cache_prev, eps: float = 1e-6, keep_cache_out: bool = True,
-                 modulation=None, fused_restore: bool = False):
-        """modulation: optional list of L dicts of per-image [B, C] bf16 tensors (adaptive LayerNorm
+                 modulation=None, fused_restore: bool = False, caches4=None, weights4=None):
+        """caches4: list of L nv.Cache4 instead of k_caches, v_caches and kv_len (which are then not looked at): keys and values in
+        4 bits, each layer as nova_pruned_block_forward_cache4 + nova_restore_from_cache. weights4: None, or a list of L f32 [B, Lmax]
+        tensors that gather the attention weight of the cached rows.
+        modulation: optional list of L dicts of per-image [B, C] bf16 tensors (adaptive LayerNorm
         of the class-conditional backbones, see nova_pruned_block_forward_adaln).
         fused_restore: with a layer_hook or select_ent, run each layer as one nova_pruned_layer_forward call instead of
         nova_pruned_block_forward + nova_restore_from_cache. The results are bit-identical; otherwise
@@ -42,6 +45,7 @@ class PrunedScaleRunner:
         self.n_heads, self.Lmax = n_heads, Lmax
         self.weights = [wt if isinstance(wt, nv.BlockWeights) else nv.BlockWeights(wt, eps) for wt in weights]
         self.k_caches, self.v_caches, self.kv_len = k_caches, v_caches, kv_len
+        self.caches4, self.weights4 = caches4, weights4
         self.cache_prev = cache_prev
         N, Cc, L = self.N, self.C, self.L
         self.ent = torch.empty((L, B, N), dtype=torch.float32, device=dev)
@@ -55,7 +59,10 @@ class PrunedScaleRunner:
         self.cache_out = (list(torch.empty((L, B, N, Cc), dtype=torch.bfloat16, device=dev).unbind(0))
                           if keep_cache_out else None)
         shape = nv.BlockShape(B, N, Cc, n_heads, self.F, Lmax, B * N)
-        ctx.ensure_workspace(shape)
+        if caches4 is not None:
+            ctx.ensure_block_cache4_workspace(shape)
+        else:
+            ctx.ensure_workspace(shape)
         self.call = nv.ScaleCall(ctx, shape, h, w, L, self.ent, self.mean, self.mean_host, self.keep_idx, self.prune_idx,
                                  self.cu_keep, self.x_buf)
         self.last_keep = None
@@ -81,7 +88,7 @@ class PrunedScaleRunner:
         j's launches (info: dict of the tensors involved); for tests that compare layer by layer.
         """
         st = stream if stream is not None else torch.cuda.current_stream()
-        if layer_hook is not None or select_ent is not None or not self.call.set_layers(
+        if layer_hook is not None or select_ent is not None or self.caches4 is not None or not self.call.set_layers(
                 self.weights, self.modulation, self.k_caches, self.v_caches, self.kv_len, self.cache_prev, self.cache_out):
             return self._run_layer_by_layer(x_in, layer_logits, sched, t, hbar_scale, append_kv, st, logits_ready, select_ent,
                                             layer_hook)
@@ -139,12 +146,22 @@ class PrunedScaleRunner:
                 x_out = self.x_buf[(j & 1) ^ (x.data_ptr() == self.x_buf[j & 1].data_ptr())]
                 cache_out = self.cache_out[j] if self.cache_out is not None else None
                 info = dict(x_in=x, x_out=x_out, cache_out=cache_out, keep=keep, keep_idx=keep_idx, prune_idx=prune_idx,
-                            cu_keep=cu_keep, k_cache=self.k_caches[j], v_cache=self.v_caches[j], kv_len=self.kv_len[j],
-                            cache_prev=self.cache_prev[j], ent=self.ent[j], stream=st)
+                            cu_keep=cu_keep, cache_prev=self.cache_prev[j], ent=self.ent[j], stream=st)
+                if self.caches4 is None:
+                    info.update(k_cache=self.k_caches[j], v_cache=self.v_caches[j], kv_len=self.kv_len[j])
+                else:
+                    info.update(cache4=self.caches4[j], kv_len=self.caches4[j].kv_len)
                 if layer_hook is not None:
                     layer_hook("before", j, info)
                 mod = self.modulation[j] if self.modulation else None
-                if self.fused_restore:
+                if self.caches4 is not None:
+                    y = self.y_kept[:M]
+                    nv.nova_pruned_block_forward_cache4(ctx, self.weights[j], shape, x, keep_idx, cu_keep, self.caches4[j], append_kv, y,
+                                                        weight=self.weights4[j] if self.weights4 is not None else None, modulation=mod,
+                                                        stream=st)
+                    nv.nova_restore_from_cache(ctx, x, y, keep_idx, prune_idx, cu_keep, self.cache_prev[j], self.h, self.w, x_out,
+                                               cache_out, stream=st)
+                elif self.fused_restore:
                     nv.nova_pruned_layer_forward(ctx, self.weights[j], mod, shape, x, keep_idx, prune_idx, cu_keep, self.k_caches[j],
                                                  self.v_caches[j], self.kv_len[j], append_kv, self.cache_prev[j],
                                                  self.h, self.w, x_out, cache_out, stream=st)
@@ -168,13 +185,18 @@ class MultiScaleRunner:
     residual cache written at the previous scale (Eq. 15; read, resized, at the next one, Eq. 16)
     and, per image, the history of scale mean entropies that the trigger of Eq. 8-10 works on. A
     scale that is not pruned yet is simply the same call sequence with every token kept.
+    With cache_bits=4 the K/V caches hold 4 bits a channel, and cache_budget bounds their rows.
     The backbone around the layers (token embedding, sampling) is not part of this library: the
     caller supplies each scale's layer input and logits.
     """
 
     def __init__(self, ctx: nv.Context, weights, n_heads: int, B: int, scales, eps: float = 1e-6,
-                 on_device: bool = False, fused_restore: bool = False):
-        """on_device: keep the entropy history and every keep count in device memory and run each
+                 on_device: bool = False, fused_restore: bool = False, cache_bits: int = 16, cache_budget: int | None = None,
+                 cache_recent: int | None = None):
+        """cache_bits=4: keys and values in 4 bits (nv.Cache4), not with on_device. cache_budget, with 4 bits: after every scale each
+        layer's cache is brought back to at most this many rows per image, the last cache_recent of them (default: as many as the
+        scale has tokens) and the others with the highest attention weight so far; None keeps all rows.
+        on_device: keep the entropy history and every keep count in device memory and run each
         scale through DeviceScaleRunner (no host synchronisation inside a scale)."""
         self.ctx, self.weights, self.n_heads, self.B, self.eps = ctx, weights, n_heads, B, eps
         self.on_device = on_device
@@ -185,9 +207,26 @@ class MultiScaleRunner:
         self.Lmax = sum(s * s for s in self.scales)
         dev = weights[0]["w_o"].device
         self.block_weights = [nv.BlockWeights(wt, eps) for wt in weights]
-        kv = torch.zeros((2 * self.L, B, self.Lmax, self.C), dtype=torch.bfloat16, device=dev).unbind(0)
-        self.k_caches, self.v_caches = list(kv[: self.L]), list(kv[self.L:])
-        self.kv_len = torch.zeros((self.L, B), dtype=torch.int32, device=dev)
+        assert cache_bits in (4, 16) and (cache_bits == 4 or cache_budget is None), "a row budget is for caches in 4 bits"
+        assert cache_bits == 16 or not on_device, "caches in 4 bits go with keep counts decided on the host"
+        self.cache_budget, self.cache_recent = cache_budget, cache_recent
+        self.caches4 = self.weights4 = self.k_caches = self.v_caches = self.kv_len = None
+        if cache_bits == 4:
+            if cache_budget is not None:
+                assert cache_budget > 0 and (cache_recent is None or 0 <= cache_recent <= cache_budget)
+                self.Lmax = min(self.Lmax, cache_budget + max(s * s for s in self.scales))
+            self.caches4 = [nv.Cache4.empty(B, self.Lmax, self.C, n_heads, dev) for _ in range(self.L)]
+            if cache_budget is not None:
+                # one more of each: an evicted layer's rows go there, and its old memory is the next layer's
+                self._spare = nv.Cache4.empty(B, self.Lmax, self.C, n_heads, dev)
+                self.weights4 = [torch.zeros((B, self.Lmax), dtype=torch.float32, device=dev) for _ in range(self.L)]
+                self._spare_weight = torch.zeros((B, self.Lmax), dtype=torch.float32, device=dev)
+                self._src_row = torch.empty((B, min(cache_budget, self.Lmax)), dtype=torch.int32, device=dev)
+        else:
+            kv = torch.zeros((2 * self.L, B, self.Lmax, self.C), dtype=torch.bfloat16, device=dev).unbind(0)
+            self.k_caches, self.v_caches = list(kv[: self.L]), list(kv[self.L:])
+            self.kv_len = torch.zeros((self.L, B), dtype=torch.int32, device=dev)
+        self._rows = 0                            # no layer and image holds more rows than this
         self.res_cache = [None] * self.L          # previous scale's residual cache per layer, [B, h, w, C]
         self.hbar_scale = torch.zeros((B, 0), dtype=torch.float32)
         self.hist_dev = torch.zeros((len(self.scales), B), dtype=torch.float32, device=dev) if on_device else None
@@ -219,8 +258,8 @@ class MultiScaleRunner:
         mean = torch.empty((B,), dtype=torch.float32, device=x_in.device)
         runner = PrunedScaleRunner(self.ctx, self.block_weights, self.n_heads, B, side, side, self.Lmax, self.k_caches,
                                    self.v_caches, self.kv_len, self.res_cache, eps=self.eps,
-                                   fused_restore=self.fused_restore)
-        same_layout = layer_hook is None and scale_logits.dtype == layer_logits[0].dtype and \
+                                   fused_restore=self.fused_restore, caches4=self.caches4, weights4=self.weights4)
+        same_layout = layer_hook is None and self.caches4 is None and scale_logits.dtype == layer_logits[0].dtype and \
             scale_logits.shape == layer_logits[0].shape and scale_logits.stride() == layer_logits[0].stride()
         if same_layout:
             # the scale's own map in the same native call: its means complete the history there
@@ -234,7 +273,20 @@ class MultiScaleRunner:
         self.hbar_scale = hbar
         x_out, keeps = runner.run_scale(x_in, layer_logits, sched, t, hbar, stream=st, layer_hook=layer_hook)
         self.res_cache = [c.view(B, side, side, self.C) for c in runner.cache_out]
+        self._rows += max(int(k.max()) for k in keeps)
+        if self.cache_budget is not None and self._rows > self.cache_budget:
+            self._evict(self.cache_recent if self.cache_recent is not None else min(N, self.cache_budget), st)
         return x_out, keeps, runner
+
+    def _evict(self, recent: int, st):
+        """Every layer's cache back to the budget."""
+        budget = self._src_row.shape[1]
+        for j in range(self.L):
+            nv.nova_cache4_evict(self.ctx, self.caches4[j], self.weights4[j], budget, min(recent, budget), self._spare,
+                                 weight_out=self._spare_weight, src_row=self._src_row, stream=st)
+            self.caches4[j], self._spare = self._spare, self.caches4[j]
+            self.weights4[j], self._spare_weight = self._spare_weight, self.weights4[j]
+        self._rows = budget
 
 
 class DeviceScaleRunner:
