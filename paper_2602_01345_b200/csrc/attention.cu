@@ -388,8 +388,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
     uint64_t* o_empty = o_full + 1;                   // 1 *, one arrival per epilogue warp
     uint64_t* m_full = o_empty + 1;                   // kSlots, one arrival per warp of the first tile's warpgroup
     uint64_t* l_full = m_full + kSlots;               // kSlots, one arrival per softmax warp
-    uint64_t* r_full = l_full + kSlots;               // Q4: kRing, one arrival per loading thread and one more
-    uint64_t* r_empty = r_full + L::kRing;            // Q4: kRing, one arrival per warp of the tile's decoding warpgroup
+    uint64_t* r_full = l_full + kSlots;               // Q4: kRing, the codes (one arrival and the bytes of the tensor maps)
+    uint64_t* rs_full = r_full + L::kRing;            // Q4: kRing, the scales (one arrival per loading thread's copies)
+    uint64_t* r_empty = rs_full + L::kRing;           // Q4: kRing, one arrival per warp of the tile's decoding warpgroup
     uint32_t* tmem_slot = (uint32_t*)(r_empty + L::kRing);
     __shared__ int ring_s[Q4 ? L::kRing : 1];         // Q4: what a ring slot brings: 1 keys, 2 values; at the end of a round -1 - stages so far
     __shared__ int abort_flag_s;
@@ -415,7 +416,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
         mbar_init(o_full, 1);
         mbar_init(o_empty, 4 * L::kCtas);
         for (int i = 0; i < kSlots; ++i) { mbar_init(&m_full[i], 4); mbar_init(&l_full[i], 8); }
-        for (int i = 0; Q4 && i < L::kRing; ++i) { mbar_init(&r_full[i], 64 + 1); mbar_init(&r_empty[i], 4); }
+        for (int i = 0; Q4 && i < L::kRing; ++i) { mbar_init(&r_full[i], 1); mbar_init(&rs_full[i], 64); mbar_init(&r_empty[i], 4); }
         fence_barrier_init();
         prefetch_tmap(&tmap_q);
         prefetch_tmap(&tmap_k);
@@ -760,7 +761,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         };
                         if (has_k) copy_rows(to_k, k_sc, yk, std::integral_constant<int, L::kKRows>(), std::integral_constant<int, DH / 16>());
                         if (has_v) copy_rows(to_v, sv, yv, std::integral_constant<int, BKV>(), std::integral_constant<int, L::kVCols / 16>());
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[rs])) : "memory");
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&rs_full[rs])) : "memory");
                         if (has_k) {
                             k_y += BKV;
                             if (s_step()) enter_k();
@@ -1135,6 +1136,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                 int done = 0;
                 while (true) {
                     ok = mbar_wait_warp(&r_full[rs], rpar, abort_flag, p.status);
+                    ok = ok && mbar_wait_warp(&rs_full[rs], rpar, abort_flag, p.status);
                     if (!ok) break;
                     const uint8_t* from = smem + L::kRingOff + rs * L::kRingBytes;
                     const int what = *(volatile int*)&ring_s[rs];
@@ -1151,11 +1153,16 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         ksc[h] = *(const uint32_t*)(from + 2 * L::kCodeBytes + k_row * (DH / 16) + (k_slab + h) * 4);
                         vsc[h] = *(const uint32_t*)(from + 2 * L::kCodeBytes + L::kScaleBytes + dt * (L::kVCols / 16) + h * 4);
                     }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&r_empty[rs]);
-                    next_ring();
+                    // (after the slot's data have been used: an arrival right behind the loads was seen before they had read, and the next
+                    // tile's copy got in between)
+                    auto release = [&]() {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&r_empty[rs]);
+                        next_ring();
+                    };
                     if (what < 0) {
                         done = -1 - what;
+                        release();
                         break;
                     }
                     if (n >= kStages) ok = mbar_wait_warp(&kv_empty[st], spar, abort_flag, p.status);
@@ -1176,6 +1183,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                         if (what & 1) put(k_to + h * L::kKRows * 128, k_row, kw[2 * h], kw[2 * h + 1], ksc[h]);
                         if (what & 2) put(v_to + h * kSlabBytes, dt, vw[2 * h], vw[2 * h + 1], vsc[h]);
                     }
+                    release();
                     fence_proxy_async_smem();
                     __syncwarp();
                     // (the fence hands the stage to the tensor core; a release at cluster scope would wait for much more: 1095 -> 904 us)

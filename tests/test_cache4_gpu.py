@@ -275,6 +275,46 @@ def test_attention_many_images(ctx, C, heads, rows):
     _check_attention(ctx, lens, counts, C, heads, seed=2)
 
 
+@pytest.mark.parametrize("C,heads,lens,rows", [(1920, 30, [1779] * 4, [563] * 4), (1920, 30, [1779, 1571, 1364, 1156], [366, 432, 497, 563]),
+                                               (1920, 15, [1500] * 4, [700] * 4), (2048, 16, [900] * 30, [100] * 30), (2048, 16, [700] * 30, [9] * 30),
+                                               (1536, 24, [640] * 30, [100] * 30)])
+def test_attention_many_work_items(ctx, C, heads, lens, rows):
+    """Several work items per CTA, one after the other, the same bits in every launch. (Against 64 bits on the device.)"""
+    cache = nova.Cache4.empty(len(lens), max(lens), C, heads)
+    g = torch.Generator(device=DEV).manual_seed(C + heads)
+    k, v = ((torch.randn((sum(lens), C), generator=g, device=DEV) * torch.exp(0.4 * torch.randn((1, C), generator=g, device=DEV))).to(torch.bfloat16)
+            for _ in range(2))
+    nova.nova_cache4_append(ctx, cache, k, v, _cu(lens))
+    kv = torch.empty((2, sum(lens), C), dtype=torch.bfloat16, device=DEV)
+    nova.nova_cache4_read(ctx, cache, _cu(lens), kv[0], kv[1])
+    m, dh = sum(rows), C // heads
+    q = (1.3 * torch.randn((m, C), generator=g, device=DEV) * torch.exp(0.5 * torch.randn((m, 1), generator=g, device=DEV))).to(torch.bfloat16)
+    ctx.ensure_cache4_workspace(cache, m)
+    runs = []
+    for _ in range(8):
+        o, lse = torch.full((m, C), 5.0, dtype=torch.bfloat16, device=DEV), torch.full((heads, m), 5.0, device=DEV)
+        nova.nova_cache4_attention(ctx, cache, q, _cu(rows), o, lse=lse)
+        runs.append((o, lse))
+    assert ctx.device_status() == 0
+    at, r0 = 0, 0
+    for n, r in zip(lens, rows):
+        qh = q[r0:r0 + r].double().view(r, heads, dh).transpose(0, 1)
+        kh, vh = (t[at:at + n].double().view(n, heads, dh).transpose(0, 1) for t in kv)
+        s = qh @ kh.transpose(1, 2) / math.sqrt(dh)
+        size = (qh.abs() @ kh.abs().transpose(1, 2)).amax(-1) / math.sqrt(dh)
+        lse, p = torch.logsumexp(s, -1), torch.softmax(s, -1)
+        # as in _ref_attention
+        delta = size * (dh * 2.0 ** -23) + (size + s.amax(-1).abs()) * 2.0 ** -21 + 2.0 ** -20
+        o, mass = p @ vh, p @ vh.abs()
+        tol = 2.0 ** -8 * (mass + o.abs()) * 1.01 + 2.0 * delta[..., None] * mass + 2.0 ** -78 * vh.abs().sum(1, keepdim=True)
+        got_o = runs[0][0][r0:r0 + r].double().view(r, heads, dh).transpose(0, 1)
+        assert ((got_o - o).abs() <= tol).all()
+        assert ((runs[0][1][:, r0:r0 + r].double() - lse).abs() <= delta + lse.abs() * 2.0 ** -22 + n * 2.0 ** -24).all()
+        at, r0 = at + n, r0 + r
+    for o, lse in runs[1:]:
+        assert torch.equal(o, runs[0][0]) and torch.equal(lse, runs[0][1])
+
+
 @pytest.mark.parametrize("rows", [1, 24, 200])
 @pytest.mark.parametrize("C,heads", [(64, 1), (128, 1)])
 def test_attention_long_cache(ctx, C, heads, rows):
