@@ -588,7 +588,7 @@ nova_status nova_cache4_read(nova_ctx* ctx, const nova_cache4* c, const int32_t*
 
 /*
  * o = softmax(q K^T / sqrt(dh)) V per head, without mask: the queries of image b attend to its rows [0, kv_len[b]).
- * q device bf16 [M, C] with row stride ldq; o device bf16 [M, C] contiguous; lse device f32 [n_heads, M] or NULL: the natural
+ * q device bf16 [M, C] with row stride ldq; o device bf16 [M, C] contiguous, not overlapping q; lse device f32 [n_heads, M] or NULL: the natural
  * logarithm of the sum of the exponentials of the scores. Queries of an image without rows get o = 0 and lse = -inf.
  * Products of bf16 operands with fp32 accumulation, probabilities rounded to bf16 for the product with V. The order of the sums
  * follows from the sizes, the counts and the SM count.
@@ -612,7 +612,7 @@ nova_status nova_cache4_weights(nova_ctx* ctx, const nova_cache4* c, const void*
  * [B, dst->Lmax] or NULL): the weights of the rows that stayed, then zeros, so that rows appended later start from nothing;
  * src_row (device int32 [B, budget] or NULL): the old row of each new one, then -1 (with NULL the list takes B * budget * 4 bytes of the
  * workspace). weight device f32 [B, Lmax]: entries below kv_len[b] must not be NaN. c itself is left as it is.
- * Errors: budget > dst->Lmax -> SHAPE; shared memory between the two caches or the weights -> INVALID_ARG.
+ * Errors: budget > dst->Lmax -> SHAPE; memory shared between what is read and what is written -> INVALID_ARG.
  */
 nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* weight, int budget, int recent,
                               const nova_cache4* dst, float* weight_out, int32_t* src_row, void* stream);

@@ -264,8 +264,10 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     r.n = 0;
     r.empty = 0;
     r.over = 0;
+    // (Q4: no row at or past M, whatever the list says)
+    auto start = [&](int i) { return Q4 ? min(cu[i], p.M) : cu[i]; };
     int units = 0;
-    for (int i = 0; i < p.B; ++i) units += (cu[i + 1] - cu[i] + kRows - 1) / kRows;
+    for (int i = 0; i < p.B; ++i) units += (start(i + 1) - start(i) + kRows - 1) / kRows;
     const int items = units * p.n_heads, rem = items % p.slots;
     const bool split = p.part && rem > 0 && 2 * rem <= p.slots && rem <= p.part_slots;
     const int whole = split ? items - rem : items;
@@ -285,8 +287,8 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
     int block = item - head * units, k_b = 0;
     r.x = head * DH;
     for (r.b = 0; r.b < p.B; ++r.b) {
-        const int c0 = cu[r.b];
-        k_b = cu[r.b + 1] - c0;
+        const int c0 = start(r.b);
+        k_b = start(r.b + 1) - c0;
         const int blocks = (k_b + kRows - 1) / kRows;
         if (block < blocks) { r.q_begin = c0 + block * kRows; break; }
         block -= blocks;

@@ -73,7 +73,7 @@ cache4_append_kernel(const AppendParams p)
             v[j] = p.v[r * p.ld + c[j]];
             const int b = image_of(p.cu, p.B, (int)r);
             const int c0 = p.cu[b], len = p.kv_len[b];
-            if (len >= 0 && (int)r >= c0 && (long)len + (p.cu[b + 1] - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
+            if (len >= 0 && (int)r >= c0 && (long)len + (min(p.cu[b + 1], p.M) - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
             else atomicOr(p.status, NOVA_DEV_SHAPE);
         }
     }
@@ -100,7 +100,7 @@ cache4_append_kernel(const AppendParams p)
         __syncthreads();
         if (last)
             for (int b = threadIdx.x; b < p.B; b += 256) {
-                const int len = p.kv_len[b], n = p.cu[b + 1] - p.cu[b];
+                const int len = p.kv_len[b], n = min(p.cu[b + 1], p.M) - p.cu[b];
                 if (len >= 0 && n > 0 && (long)len + n <= p.Lmax) p.kv_len[b] = len + n;
             }
     }
@@ -457,11 +457,21 @@ nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* 
     if (budget > dst->Lmax) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_evict: budget larger than the new cache");
     if (c->Lmax > (1 << 30)) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_evict: too many rows");
     if (c->B == 0) return NOVA_OK;
-    if (c->kv_len == dst->kv_len || (c->Lmax > 0 && (c->k_codes == dst->k_codes || c->v_codes == dst->v_codes || c->k_scales == dst->k_scales ||
-                                                     c->v_scales == dst->v_scales)))
-        return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_cache4_evict: the new cache must not share memory with the old one");
+    // what is written must not overlap anything that is read, or what else is written
+    const size_t rows_in = (size_t)c->B * c->Lmax, rows_out = (size_t)c->B * dst->Lmax;
+    struct { const void* p; size_t bytes; bool written; } mem[] = {
+        {c->k_codes, rows_in * (c->C / 2), false}, {c->v_codes, rows_in * (c->C / 2), false}, {c->k_scales, rows_in * (c->C / 16), false},
+        {c->v_scales, rows_in * (c->C / 16), false}, {c->kv_len, (size_t)c->B * 4, false}, {weight, rows_in * 4, false},
+        {dst->k_codes, rows_out * (c->C / 2), true}, {dst->v_codes, rows_out * (c->C / 2), true}, {dst->k_scales, rows_out * (c->C / 16), true},
+        {dst->v_scales, rows_out * (c->C / 16), true}, {dst->kv_len, (size_t)c->B * 4, true}, {weight_out, rows_out * 4, true},
+        {src_row, (size_t)c->B * budget * 4, true}};
+    const int n_mem = (int)(sizeof(mem) / sizeof(mem[0]));
+    for (int i = 0; i < n_mem; ++i)
+        for (int j = 0; j < i; ++j)
+            if (mem[i].written && mem[i].p && mem[j].p && mem[i].bytes && mem[j].bytes &&
+                (uintptr_t)mem[i].p < (uintptr_t)mem[j].p + mem[j].bytes && (uintptr_t)mem[j].p < (uintptr_t)mem[i].p + mem[i].bytes)
+                return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_cache4_evict: the new cache, its weights or the list overlap other memory of the call");
     if (c->Lmax > 0 && !weight) return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_cache4_evict: null weights");
-    if (weight && weight == weight_out) return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_cache4_evict: weight_out aliases weight");
     if (!aligned4(weight) || !aligned4(weight_out) || !aligned4(src_row))
         return nova_fail(ctx, NOVA_ERR_ALIGNMENT, "nova_cache4_evict: misaligned tensor");
     int32_t* list = src_row;

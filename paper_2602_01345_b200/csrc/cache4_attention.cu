@@ -95,7 +95,7 @@ struct FewWalk {
     // (an image without keys has none: its rows are written by fill_empty)
     __device__ __forceinline__ static int image_units(const FewParams& p, int b)
     {
-        return image_len(p, b) == 0 ? 0 : (max(p.cu[b + 1] - p.cu[b], 0) + kFewRows - 1) / kFewRows * p.n_heads;
+        return image_len(p, b) == 0 ? 0 : (max(min(p.cu[b + 1], p.M) - p.cu[b], 0) + kFewRows - 1) / kFewRows * p.n_heads;
     }
     __device__ __forceinline__ static int image_len(const FewParams& p, int b)
     {
@@ -611,6 +611,7 @@ nova_status nova_cache4_attention(nova_ctx* ctx, const nova_cache4* c, const voi
     if (rc != NOVA_OK) return rc;
     if (M == 0 || c->B == 0) return NOVA_OK;
     if (((uintptr_t)lse) & 3u) return nova_fail(ctx, NOVA_ERR_ALIGNMENT, "nova_cache4_attention: misaligned lse");
+    if (o == q) return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "nova_cache4_attention: o aliases q");
     NOVA_DEVICE_GUARD(ctx, "nova_cache4_attention");
     cudaStream_t st = (cudaStream_t)stream;
     rc = nova_debug_check_lists(ctx, "nova_cache4_attention", nullptr, nullptr, cu_q, c->B, M, M, false, st);

@@ -218,7 +218,7 @@ nova_status nova_launch_cache4_weights(nova_ctx* ctx, const nova_cache4* c, cons
     // as many parts as bring the launch to kWtWaves CTAs per SM (two run at once; the images' lengths differ), no more than there can
     // be (head, chunk) pairs
     const long pairs = (long)c->n_heads * (((long)M + kWtChunk - 1) / kWtChunk);
-    p.parts = (int)max(1l, min(pairs, (long)kWtWaves * ctx->num_sms / whole));
+    p.parts = whole > NOVA_TICKETS ? 1 : (int)max(1l, min(pairs, (long)kWtWaves * ctx->num_sms / whole));
     if (whole * p.parts > 0x7fffffffL) return nova_fail(ctx, NOVA_ERR_SHAPE, "nova_cache4_weights: too many rows");
     if (p.parts > 1 && (!scratch || scratch_bytes < nova_cache4_weights_scratch(ctx->num_sms)))
         return nova_fail(ctx, NOVA_ERR_WORKSPACE, "nova_cache4_weights: workspace missing or too small");

@@ -76,7 +76,8 @@ def test_bad_rows(ctx, k, cu, m, ld, status):
 
 def test_bad_vectors(ctx):
     c = C.byref(_cache())
-    assert nv._lib.nova_cache4_attention(ctx, c, FAKE, 128, FAKE, 4, FAKE, FAKE + 2, None) == 3
+    assert nv._lib.nova_cache4_attention(ctx, c, FAKE, 128, FAKE, 4, 2 * FAKE, FAKE + 2, None) == 3
+    assert nv._lib.nova_cache4_attention(ctx, c, FAKE, 128, FAKE, 4, FAKE, None, None) == 1      # in place
     assert nv._lib.nova_cache4_weights(ctx, c, FAKE, 128, None, FAKE, 4, None, FAKE, None) == 1
     assert nv._lib.nova_cache4_weights(ctx, c, FAKE, 128, FAKE, FAKE, 4, None, None, None) == 1
     assert nv._lib.nova_cache4_weights(ctx, c, FAKE, 128, FAKE, None, 0, None, FAKE, None) == 1
@@ -93,6 +94,9 @@ def test_bad_evictions(ctx):
     assert evict(dst=dict(B=3)) == 1 and evict(dst=dict(C=192)) == 2 and evict(dst=dict(C=256)) == 1 and evict(dst=dict(n_heads=1)) == 1
     assert evict(weight=None) == 1 and evict(w_out=20 * FAKE) == 1
     assert evict(weight=20 * FAKE + 2) == 3 and evict(w_out=22 * FAKE + 1) == 3 and evict(rows=21 * FAKE + 2) == 3
+    # memory that overlaps without starting at the same place: 2 * 64 rows of 64 bytes of codes, of 8 of scales, 512 bytes of weights
+    assert evict(dst=dict(k_codes=FAKE + 2 * 64 * 64 - 16)) == 1 and evict(dst=dict(v_scales=4 * FAKE - 2 * 64 * 8 + 16)) == 1
+    assert evict(w_out=20 * FAKE + 2 * 64 * 4 - 4) == 1 and evict(rows=11 * FAKE + 64) == 1 and evict(rows=15 * FAKE) == 1
     for shared in ("k_codes", "v_codes", "k_scales", "v_scales", "kv_len"):
         assert evict(dst={shared: getattr(_cache(), shared)}) == 1
     if not torch.cuda.is_available():
