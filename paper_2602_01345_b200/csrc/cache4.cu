@@ -44,12 +44,27 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& x, uint16_t& scale)
     // or at least 2^-10 from one. Rounded to a multiple of 2^-11 (the multiply-add's sum has no finer bits), a half comes out as
     // exactly that, and everything else stays on its side of it; the second sum rounds to a whole number, ties to even, in the low bits.
     const float inv = __frcp_rn(s);
-    auto code = [&](float x) { return __float_as_uint(__fadd_rn(__fadd_rn(__fmaf_rn(x, inv, 6144.f), -6144.f), 12582920.f)) & 15u; };      // 1.5 2^23 + 8
-    uint32_t out = 0;
+    uint64_t inv2, grid2, back2, whole2;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(inv2) : "f"(inv));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(grid2) : "f"(6144.f));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(back2) : "f"(-6144.f));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(whole2) : "f"(12582920.f));          // 1.5 2^23 + 8
+    uint32_t even[4], odd[4];          // codes plus 8 in the low byte
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        out |= code(__uint_as_float(w[i] << 16)) << (4 * i) | code(__uint_as_float(w[i] & 0xffff0000u)) << (16 + 4 * i);
-    return out;
+    for (int i = 0; i < 4; ++i) {
+        uint64_t x;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(w[i] << 16), "r"(w[i] & 0xffff0000u));
+        asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(x) : "l"(inv2), "l"(grid2));
+        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(back2));
+        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(whole2));
+        asm("mov.b64 {%0, %1}, %2;" : "=r"(even[i]), "=r"(odd[i]) : "l"(x));
+    }
+    // four bytes of codes to four nibbles, in bytes 0 and 2
+    auto nibbles = [](const uint32_t (&u)[4]) {
+        const uint32_t b = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+        return b | b >> 4;
+    };
+    return __byte_perm(nibbles(even), nibbles(odd), 0x6420);
 }
 
 __global__ void __launch_bounds__(256)
@@ -62,6 +77,7 @@ cache4_append_kernel(const AppendParams p)
     uint4 k[kPer], v[kPer];
     long dst[kPer];
     unsigned c[kPer];
+    int b = 0, c0 = 0, c1 = 0, len = -1;                 // the image of the last row looked up
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const unsigned i = blockIdx.x * (256u * kPer) + j * 256u + threadIdx.x, r = i / vec;
@@ -71,9 +87,13 @@ cache4_append_kernel(const AppendParams p)
         if (r < (unsigned)rows) {
             k[j] = p.k[r * p.ld + c[j]];
             v[j] = p.v[r * p.ld + c[j]];
-            const int b = image_of(p.cu, p.B, (int)r);
-            const int c0 = p.cu[b], len = p.kv_len[b];
-            if (len >= 0 && (int)r >= c0 && (long)len + (min(p.cu[b + 1], p.M) - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
+            if (j == 0 || (int)r >= c1) {
+                b = image_of(p.cu, p.B, (int)r);
+                c0 = p.cu[b];
+                c1 = p.cu[b + 1];
+                len = p.kv_len[b];
+            }
+            if (len >= 0 && (int)r >= c0 && (long)len + (min(c1, p.M) - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
             else atomicOr(p.status, NOVA_DEV_SHAPE);
         }
     }
