@@ -39,6 +39,17 @@
 // table, loads, S, softmax, O. Measured against the kernel before it (two tiles of one item in a CTA), us:
 // 3277 rows x 29414 keys, 16 heads x 128: 684 -> 572; 4 x 2048 x 8473: 510 -> 416; 1024 x 7449: 86 -> 52;
 // 300 x 821: 22.8 -> 12.5; 4 x 563 x 1779, 30 heads x 64: 80 -> 55; 2 x 128 x 552, 16 x 64: 11.8 -> 9.2.
+//
+// With the cache in 4 bits (Q4) two warpgroups more stand between the cache and the stages: warps 2 and 3 bring packed tiles to a ring in
+// shared memory, warps 16 to 23 decode them into the stages, exactly, so that everything behind a stage is as above. What differs:
+// the last round's items are shared by as many CTAs as there are (parts of six key tiles at least) and merged by all warps of the last
+// to finish; warps of the softmax whose rows do not exist skip it; the polynomial is a quartic, since the log-sum-exp is a
+// result; and at head size 128 up to 128 rows per image go to CTAs alone, with two stages of whole tiles (64 rows x 29414 keys,
+// 16 heads: pairs 84 us, alone 67).
+// What bounds it: the schedulers, which the decoding shares with the softmax at 80 registers a thread (61 % of the issue slots in use), and
+// the hand-overs between them: 3277 rows x 29414 keys 858 us back to back, 770 after a pause, where the bf16 cache takes 572. Measured and not
+// kept: both softmax warpgroups on halves of every tile 918 us against 760; registers moved between the warpgroups (setmaxnreg) 768;
+// four stages, or a shorter ring, +-1 %.
 #include "cache4.cuh"
 
 #include <type_traits>

@@ -15,6 +15,13 @@
 // keys), while the sum takes them in fp32.
 // A fragment's channels and keys are permuted so that each thread decodes contiguous bytes: channels are the contraction of Q K^T,
 // keys that of P V, and O's columns may lie anywhere, so only Q's loads and O's stores know of it.
+// Up to kFewPerImage rows per image on average take this kernel, more the 128-row tiles of attention.cu: a second unit per head
+// decodes everything once more, where those take 128 rows for one price. us for one image, 16 heads of 128, here and there: 10 rows
+// x 512 keys 12.4 and 12.8, x 4096 16.5 and 29.9, x 29414 48 and 66; 64 rows x 29414 here (in four units) 123, there 67.
+// What bounds it: at 29414 keys 1.2 us per SM for 128 keys of a head where the bytes would take 0.42, the decoding's integer and
+// bf16 instructions and the products about 0.3 each if nothing else ran: latencies, at eight warps of 217 registers (twelve
+// of 168 are 3 % slower there and 2 us slower in small calls, sixteen 20 %). With few keys the chain of
+// lengths, keys, four steps of the warps' reduction, and, where a unit is shared, the merge (3 us).
 #include "cache4.cuh"
 
 namespace {
@@ -93,7 +100,8 @@ __device__ __forceinline__ long div_pos(long a, long b)
 }
 
 // A place in the launch's tiles: tile t of unit (b, head, block), of which the image has `units`, with T tiles each, the first of
-// which (t = 0) has no keys: key tile t - 1 otherwise. Without it CTAs whose tiles are many units of few keys ended late.
+// which (t = 0) has no keys: key tile t - 1 otherwise. It stands for what a unit costs besides its keys, about a tile's time, so
+// that CTAs whose tiles are many units of few keys do not end last.
 template <int DH>
 struct FewWalk {
     int b, unit, units, t, T, rows, len;
@@ -306,8 +314,8 @@ cache4_few_kernel(const FewParams p)
             const int key0 = (int)(tile - row0 - 1) * L::kTile + warp * kWarpKeys;
             if (tile > row0 && key0 < len) {
                 const uint8_t* s_at = ring + slot * L::kStageBytes;
-                // 16 keys at a time, in a loop that is not unrolled: the code is fetched once per launch, 16 KB in about 6 us
-                // (with 32 keys at a time, 68 KB of code in all, 47 us of a launch of 61 passed before the second tile)
+                // 16 keys at a time, in a loop that is not unrolled: unrolled it is 2 % faster for ten rows x 29414 keys and no
+                // faster for few keys, with 7 KB more code to fetch
 #pragma unroll 1
                 for (int kb = 0; kb < 2; ++kb) {
                     if (key0 + 16 * kb >= len) break;

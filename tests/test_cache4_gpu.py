@@ -412,6 +412,11 @@ def test_weights_ragged(ctx, C, heads):
     _check_weights(ctx, [130, 0, 1, 300, 77], [20, 9, 33, 0, 150], C, heads, seed=3, lmax=400, extra=4)
 
 
+def test_weights_of_many_images(ctx):
+    rng = np.random.default_rng(4)
+    _check_weights(ctx, rng.integers(0, 7, size=1100).tolist(), rng.integers(0, 3, size=1100).tolist(), 64, 1, seed=2)
+
+
 def test_weights_of_many_queries(ctx):
     _check_weights(ctx, [600, 1100], [900, 513], 256, 4, seed=5)
     _check_weights(ctx, [600, 1100], [900, 513], 256, 2, seed=6)
@@ -619,6 +624,30 @@ def test_calls_replay_from_a_graph(ctx):
         nova.nova_cache4_append(own, cache, k, v, cu, stream=side)
     side.synchronize()
     assert cache.kv_len.tolist() == [506, 170]
+
+
+@pytest.mark.parametrize("bad", [[0, 9, 4], [1, 4, 9], [0, 4, 11], [0, -3, 9]])
+def test_debug_mode_refuses_bad_row_lists(bad):
+    ctx = nova.Context(0)
+    ctx.set_debug(True)
+    C = 128
+    cache, k, v = _filled(ctx, [5, 3], 20, C, 2, 1)
+    before = [t.clone() for t in (cache.k_codes, cache.kv_len)]
+    rows = _rows(2, 10, C).to(DEV)
+    o, lse, w = torch.full_like(rows, 3.0), torch.full((2, 10), 3.0, device=DEV), torch.full((2, 20), 3.0, device=DEV)
+    out = torch.full_like(rows, 3.0)
+    ctx.ensure_cache4_workspace(cache, 10)
+    for call in (lambda: nova.nova_cache4_append(ctx, cache, rows, rows, _i32(bad)), lambda: nova.nova_cache4_read(ctx, cache, _i32(bad), o, out),
+                 lambda: nova.nova_cache4_attention(ctx, cache, rows, _i32(bad), o, lse=lse),
+                 lambda: nova.nova_cache4_weights(ctx, cache, rows, lse, _i32(bad), w)):
+        with pytest.raises(nova.NovaError) as e:
+            call()
+        assert e.value.status == 1
+    assert torch.equal(cache.k_codes, before[0]) and torch.equal(cache.kv_len, before[1])
+    for t in (o, out, lse, w):
+        assert (t == 3.0).all()
+    nova.nova_cache4_attention(ctx, cache, rows, _i32([0, 4, 10]), o, lse=lse)
+    assert ctx.device_status() == 0 and torch.isfinite(o.float()).all()
 
 
 def test_empty_calls_are_no_ops(ctx):
