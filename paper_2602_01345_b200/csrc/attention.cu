@@ -45,9 +45,9 @@
 // the last round's items are shared by as many CTAs as there are (parts of six key tiles at least) and merged by all warps of the last
 // to finish; warps of the softmax whose rows do not exist skip it; the polynomial is a quartic, since the log-sum-exp is a
 // result; and at head size 128 up to 128 rows per image go to CTAs alone, with two stages of whole tiles (64 rows x 29414 keys,
-// 16 heads: pairs 84 us, alone 67).
+// 16 heads: pairs 84 us, alone 67, 64 with the merge's loads unrolled).
 // What bounds it: the schedulers, which the decoding shares with the softmax at 80 registers a thread (61 % of the issue slots in use), and
-// the hand-overs between them: 3277 rows x 29414 keys 858 us back to back, 770 after a pause, where the bf16 cache takes 572. Measured and not
+// the hand-overs between them: 3277 rows x 29414 keys 851 us back to back, 770 after a pause, where the bf16 cache takes 572. Measured and not
 // kept: both softmax warpgroups on halves of every tile 918 us against 760; registers moved between the warpgroups (setmaxnreg) 768;
 // four stages, or a shorter ring, +-1 %.
 #include "cache4.cuh"
@@ -349,13 +349,14 @@ __device__ __noinline__ void merge_parts(const AttnParams& p, const Pass* table,
     for (; passes; passes &= passes - 1) {
         const Pass& t = table[__ffsll((long long)passes) - 1];
         const int parts = t.parts, rows = min(BQ, t.rows_valid - rank * BQ), head = t.x / DH;
-        for (int at = threadIdx.x; at < BQ * (DH / 8); at += blockDim.x) {
-            const int row = at % BQ, col = at / BQ * 8;
-            if (row >= rows) continue;
+        for (int at = threadIdx.x; at < rows * (DH / 8); at += blockDim.x) {
+            const int row = at % rows, col = at / rows * 8;
             const float* all = p.part + (long)t.part0 * kPart + rank * BQ + row;
             float top = -1e30f, l = 0.f, sum[8];
 #pragma unroll
             for (int g = 0; g < 8; ++g) sum[g] = 0.f;
+            // (unrolled, so that the loads do not wait for one another)
+#pragma unroll 8
             for (int j = 0; j < parts; ++j) top = fmaxf(top, __ldcg(all + j * kPart + DH * kRows));
 #pragma unroll 4
             for (int j = 0; j < parts; ++j) {

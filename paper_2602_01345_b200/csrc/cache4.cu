@@ -1,5 +1,5 @@
 // The 4-bit K/V cache: append (quantise), read (decode) and eviction. The format is described in cache4.cuh.
-// 8263 rows of 2048: append 24 us (86 MB; its instructions fill 80 % of the issue slots), read 17 us (86 MB). Eviction of 8 images of up to 2237
+// 8266 rows of 2048: append 24 us (86 MB; its instructions fill 80 % of the issue slots), read 17 us (86 MB). Eviction of 8 images of up to 2237
 // rows of 1920 to 1216: 10 us to choose, 10 to move; of 32 images of 10521 rows of 2048 to 4096, read back included, 362 us (1.98 GB).
 #include "cache4.cuh"
 

@@ -17,7 +17,7 @@
 // keys that of P V, and O's columns may lie anywhere, so only Q's loads and O's stores know of it.
 // Up to kFewPerImage rows per image on average take this kernel, more the 128-row tiles of attention.cu: a second unit per head
 // decodes everything once more, where those take 128 rows for one price. us for one image, 16 heads of 128, here and there: 10 rows
-// x 512 keys 12.4 and 12.8, x 4096 16.5 and 29.9, x 29414 48 and 66; 64 rows x 29414 here (in four units) 123, there 67.
+// x 512 keys 12.4 and 12.8, x 4096 16.3 and 29.9, x 29414 48 and 66; 64 rows x 29414 here (in four units) 123, there 64.
 // What bounds it: at 29414 keys 1.2 us per SM for 128 keys of a head where the bytes would take 0.42, the decoding's integer and
 // bf16 instructions and the products about 0.3 each if nothing else ran: latencies, at eight warps of 217 registers (twelve
 // of 168 are 3 % slower there and 2 us slower in small calls, sixteen 20 %). With few keys the chain of
@@ -530,6 +530,7 @@ cache4_few_kernel(const FewParams p)
             if (r < rows && r < kFewRows && row_base + r < p.M) {
                 auto part = [&](int c) { return p.part + ((long)c * 2 + (c == c0 ? 1 : 0)) * L::kSlotFloats; };
                 float top = -1e30f, sum = 0.f, o[kPer];
+#pragma unroll 8
                 for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(part(c) + kFewRows * DH + r));
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) o[i] = 0.f;

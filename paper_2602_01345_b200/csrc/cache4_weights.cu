@@ -9,8 +9,8 @@
 // which the next head's words are loaded before the present one is worked on.
 // Where there are few key tiles, the (head, query chunk) pairs of a tile are divided over several CTAs, whose sums the last of
 // them adds in the order of the parts: nothing depends on who comes first.
-// 1024 and 768 rows x 7449 and 5587 keys, 16 heads of 128: 167 us (281 TFLOP/s; mma.sync alone would take about 107 at the rate that the pipe
-// shows, the exponentials 81), 256 with two chains of products instead of four, 32 queries a chunk and two CTAs per SM in all.
+// 768 and 1024 rows x 7449 and 5587 keys, 16 heads of 128: 167 us (281 TFLOP/s; mma.sync alone would take about 107 at the rate that the
+// pipe shows, the exponentials 41), 256 with two chains of products instead of four, 32 queries a chunk and two CTAs per SM in all.
 #include "cache4.cuh"
 
 namespace {
