@@ -132,6 +132,14 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// 2^d of a difference d <= 0 of two references as the product low * rest of two normal numbers (low alone, rest = 1, from -120 up). A part of
+// the keys may hold scores up to 2^128 above its own reference, so that its sums count although 2^d by itself would be flushed to
+// zero. Multiplied one after the other, rest first, the two lose nothing that counts beside the highest part, whose sum is 2^-kHeadroom at least.
+__device__ __forceinline__ void ex2_wide(float d, float& low, float& rest)
+{
+    low = ex2(fmaxf(d, -120.f));
+    rest = ex2(fminf(d + 120.f, 0.f));
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
@@ -361,10 +369,11 @@ __device__ __noinline__ void merge_parts(const AttnParams& p, const Pass* table,
 #pragma unroll 4
             for (int j = 0; j < parts; ++j) {
                 const float* part = all + j * kPart;
-                const float f = ex2((__ldcg(part + DH * kRows) - top) * c);
-                l = fmaf(__ldcg(part + (DH + 1) * kRows), f, l);
+                float f, rest;
+                ex2_wide((__ldcg(part + DH * kRows) - top) * c, f, rest);
+                l = fmaf(__ldcg(part + (DH + 1) * kRows) * rest, f, l);
 #pragma unroll
-                for (int g = 0; g < 8; ++g) sum[g] = fmaf(__ldcg(part + (col + g) * kRows), f, sum[g]);
+                for (int g = 0; g < 8; ++g) sum[g] = fmaf(__ldcg(part + (col + g) * kRows) * rest, f, sum[g]);
             }
             const float inv = 1.f / l;
             const long r = t.q_begin + rank * BQ + row;

@@ -673,3 +673,50 @@ def test_empty_calls_are_no_ops(ctx):
     ctx.ensure_cache4_workspace(flat, 2)
     nova.nova_cache4_attention(ctx, flat, q, _cu([2]), o)
     assert (o == 0).all() and ctx.device_status() == 0
+
+
+# ---- items shared by key ranges whose scores lie far apart ------------------------------------------------------------
+def _apart(depth, C, n, half, zero):
+    """Keys of one head of C channels, and a query's channels 0 and 32 with which their scores are, in units of log2, 0 for key `zero`, -1/2 for
+    key `half` and -depth for all others."""
+    k = torch.zeros((n, C))
+    k[:, 0] = -7.0
+    k[half, 0], k[half, 32] = 0.0, -7.0
+    k[zero, 0] = 0.0
+    unit = math.log(2.0) * math.sqrt(C) / 7.0
+    return k.to(torch.bfloat16), depth * unit, 0.5 * unit
+
+
+@pytest.mark.parametrize("C", [64, 128])
+@pytest.mark.parametrize("rows", [24, 200, 300])
+@pytest.mark.parametrize("depth", [60.0, 127.0, 140.0, 200.0])
+@pytest.mark.parametrize("low_first", [True, False])
+def test_attention_ranges_far_apart_share_a_row(ctx, C, rows, depth, low_first):
+    """2500 keys are 20 tiles, shared by three CTAs (keys from 0, 768 and 1664): the range whose first tile lies `depth` below holds 0.41 of
+    the weight, in a later key. Up to about 128 it does so against that tile, beyond it the item is run again."""
+    n, heads = 2500, 1
+    half, zero = (500, 770) if low_first else (1500, 5)
+    k, q0, q32 = _apart(depth, C, n, half, zero)
+    v = _rows(2, n, C)
+    cache = nova.Cache4.empty(1, n, C, heads)
+    nova.nova_cache4_append(ctx, cache, k.to(DEV), v.to(DEV), _cu([n]))
+    q = _rows(3, rows, C)
+    q[:, :64] = 0
+    q[:, 0] = (q0 * (1.0 - 0.25 * (torch.arange(rows) % 4))).to(torch.bfloat16)
+    q[:, 32] = q32
+    ctx.ensure_cache4_workspace(cache, rows)
+    o = torch.empty((rows, C), dtype=torch.bfloat16, device=DEV)
+    lse = torch.empty((heads, rows), device=DEV)
+    nova.nova_cache4_attention(ctx, cache, q.to(DEV), _cu([rows]), o, lse=lse)
+    assert ctx.device_status() == 0
+    ref_o, ref_l, tol_o, tol_l = _ref_attention(q.double().numpy(), _ref_quantise(k)[0], _ref_quantise(v)[0], heads)
+    assert np.all(np.abs(lse.double().cpu().numpy() - ref_l) <= tol_l)
+    assert np.all(np.abs(o.double().cpu().numpy() - ref_o) <= tol_o)
+
+
+@pytest.mark.parametrize("C", [64, 128])
+@pytest.mark.parametrize("rows", [24, 200, 300])
+@pytest.mark.parametrize("q_scale", [20.0, 40.0])
+def test_attention_long_cache_scores_far_apart(ctx, C, rows, q_scale):
+    """157 tiles shared by up to 26 CTAs, with scores of hundreds: the ranges' references lie far apart, and items are run again."""
+    _check_attention(ctx, [20011], [rows], C, 1, seed=31, q_scale=q_scale)
