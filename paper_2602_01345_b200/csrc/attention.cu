@@ -922,15 +922,19 @@ attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_consta
                             // not depend on which.
                             const float m_o = __ldcg(other + DH * L::kRows), l_o = __ldcg(other + (DH + 1) * L::kRows);
                             const float m_new = fmaxf(m_ref, m_o);
-                            const float a_me = ex2((m_ref - m_new) * c), a_o = ex2((m_o - m_new) * c);
+                            float a_me, a_o, b_me, b_o;         // 2^(difference) = a * b
+                            ex2_wide((m_ref - m_new) * c, a_me, b_me);
+                            ex2_wide((m_o - m_new) * c, a_o, b_o);
                             const bool first = (khalf == 0);
                             const float a0 = first ? a_me : a_o, a1 = first ? a_o : a_me;
-                            const float l0 = first ? l_run : l_o, l1 = first ? l_o : l_run;
+                            const float b0 = first ? b_me : b_o, b1 = first ? b_o : b_me;
+                            const float l0 = (first ? l_run : l_o) * b0, l1 = (first ? l_o : l_run) * b1;
                             const float inv = 1.f / __fmaf_rn(l0, a0, __fmul_rn(l1, a1));
                             const float w0 = a0 * inv, w1 = a1 * inv;
                             const float w_me = first ? w0 : w1, w_o = first ? w1 : w0;
                             auto mix = [&](uint32_t mine_bits, float theirs) {
-                                const float v = __uint_as_float(mine_bits);
+                                const float v = __uint_as_float(mine_bits) * b_me;
+                                theirs *= b_o;
                                 // half 0's term is the multiply-add operand, half 1's the rounded product
                                 return first ? __fmaf_rn(v, w_me, __fmul_rn(theirs, w_o))
                                              : __fmaf_rn(theirs, w_o, __fmul_rn(v, w_me));

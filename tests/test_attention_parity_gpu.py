@@ -559,3 +559,50 @@ def test_block_variants_match_oracle(ctx, parts, C, heads):
     if on_device:
         assert torch.isnan(y[M:].float()).all()
     assert kv_len.cpu().tolist() == [a + b for a, b in zip(kv_lens, ks)]
+
+
+@pytest.mark.parametrize("C", [64, 128])
+@pytest.mark.parametrize("rows", [24, 300])
+@pytest.mark.parametrize("depth", [60.0, 127.0, 140.0, 200.0])
+@pytest.mark.parametrize("low_first", [True, False])
+def test_attention_halves_far_apart_share_a_row(ctx, C, rows, depth, low_first):
+    """One head, every query the same: one key of each half of a split item scores 0 and -1/2 (in units of log2), all others -depth, the first
+    tile of the half with -1/2 among them. That half holds 0.41 of the weight: against its own first tile up to about 128, beyond it the
+    item is run again. (Queries and new keys and values are the biases: the weights of the projection are zero.)"""
+    F, n, dh = 2048, 2500, C                      # (F: room in the workspace for the halves' results)
+    Lmax = n + rows
+    tiles = -(-Lmax // 128)
+    second = -(-tiles // 2) * 128                 # first key of the second half
+    half, zero = (700, second + 3) if low_first else (second + 700, 3)
+    wt = probe_weights(C, F, 7)
+    wt["w_qkv"].zero_()
+    unit = np.log(2.0) * np.sqrt(dh) / 8.0
+    q = torch.zeros(C, dtype=torch.bfloat16)
+    q[0], q[32] = depth * unit, 0.5 * unit
+    k = torch.zeros((Lmax, C), dtype=torch.bfloat16)
+    k[:, 0] = -8.0
+    k[half, 0], k[half, 32] = 0.0, -8.0
+    k[zero, 0] = 0.0
+    g = torch.Generator(device="cpu").manual_seed(3)
+    v = torch.randn((Lmax, C), generator=g).to(torch.bfloat16)
+    v[n:] = v[n]
+    wt["b_qkv"].copy_(torch.cat((q, k[n], v[n])).to(DEV))
+    k_cache, v_cache = (torch.cat((t[:n], torch.full((rows, C), float("nan"), dtype=torch.bfloat16)))[None].contiguous().to(DEV) for t in (k, v))
+    x = torch.zeros((1, rows, C), dtype=torch.bfloat16, device=DEV)
+    shape = nova.BlockShape(1, rows, C, 1, F, Lmax, rows)
+    ctx.ensure_workspace(shape)
+    y = torch.empty((rows, C), dtype=torch.bfloat16, device=DEV)
+    nova.nova_pruned_block_forward(ctx, nova.BlockWeights(wt, 1e-6), shape, x, torch.arange(rows, dtype=torch.int32, device=DEV),
+                                   torch.tensor([0, rows], dtype=torch.int32, device=DEV), k_cache, v_cache,
+                                   torch.tensor([n], dtype=torch.int32, device=DEV), True, y)
+    assert ctx.device_status() == 0
+    s = k.double().numpy() @ q.double().numpy() / np.sqrt(dh)
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    v64 = v.double().numpy()
+    o, mass = p @ v64, p @ np.abs(v64)
+    # Rounding of probabilities and of o to bf16: 2^-8 each; a probability by the cubic, 9.2e-5, twice (it is also in the sum); a score of up to
+    # depth log2 units and its reference to 2^-22 of their size. Both results are exact sums of two products before that.
+    tol = 2.0 ** -8 * (mass + np.abs(o)) * 1.01 + 2.0 * (9.2e-5 + (depth + 48.0) * 2.0 ** -21) * mass
+    assert 0.4 < p[half] < 0.43
+    assert (np.abs(y.double().cpu().numpy() - o) <= tol).all()
