@@ -622,7 +622,8 @@ nova_status nova_cache4_evict(nova_ctx* ctx, const nova_cache4* c, const float* 
  * written behind the cache's rows, and the queries attend to all of them as they are held (Eq. 14 with the values of the 4-bit rows).
  * cache: B, C, n_heads and Lmax as in s. append_kv != 0 advances its kv_len. weight: NULL, or device f32 [B, Lmax] (then
  * append_kv must not be 0): the weights that this call's queries give to the rows, its own among them, are added; entries at or past
- * kv_len[b] must be zero before. An image whose rows do not fit in Lmax records NOVA_ERR_SHAPE as in nova_cache4_append.
+ * kv_len[b] must be zero before. An image whose rows do not fit in Lmax records NOVA_ERR_SHAPE as in nova_cache4_append: its rows,
+ * length and weights stay as they were, and its y is that of queries that attend to the rows it has; other images are not affected.
  * Workspace: nova_block_cache4_workspace_bytes. Everything else, errors included, as for the other block calls.
  */
 size_t      nova_block_cache4_workspace_bytes(const nova_ctx* ctx, const nova_block_shape* s);

@@ -313,7 +313,7 @@ __device__ __forceinline__ Pass make_pass(const AttnParams& p, const int32_t* cu
         block -= blocks;
     }
     r.rows_valid = min(kRows, k_b - block * kRows);
-    const int n_keys = min(max(len[r.b], 0) + (p.own_keys ? k_b : 0), p.Lmax);
+    const int n_keys = Q4 ? c4::keys_of(len[r.b], k_b, p.own_keys, p.Lmax) : min(max(len[r.b], 0) + (p.own_keys ? k_b : 0), p.Lmax);
     const int tiles = (n_keys + BKV - 1) / BKV;
     if constexpr (Q4) {
         if (khalf >= 0) {

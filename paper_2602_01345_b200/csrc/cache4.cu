@@ -95,7 +95,7 @@ cache4_append_kernel(const AppendParams p)
                 c1 = p.cu[b + 1];
                 len = p.kv_len[b];
             }
-            if (len >= 0 && (int)r >= c0 && (long)len + (min(c1, p.M) - c0) <= p.Lmax) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
+            if ((int)r >= c0 && rows_fit(len, min(c1, p.M) - c0, p.Lmax)) dst[j] = (long)b * p.Lmax + len + ((int)r - c0);
             else atomicOr(p.status, NOVA_DEV_SHAPE);
         }
     }
@@ -123,7 +123,7 @@ cache4_append_kernel(const AppendParams p)
         if (last)
             for (int b = threadIdx.x; b < p.B; b += 256) {
                 const int len = p.kv_len[b], n = min(p.cu[b + 1], p.M) - p.cu[b];
-                if (len >= 0 && n > 0 && (long)len + n <= p.Lmax) p.kv_len[b] = len + n;
+                if (n > 0 && rows_fit(len, n, p.Lmax)) p.kv_len[b] = len + n;
             }
     }
 }

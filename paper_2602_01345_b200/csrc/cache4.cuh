@@ -56,6 +56,14 @@ __device__ __forceinline__ void decode8(uint32_t w, const Scale2& s, uint32_t (&
     out[3] = value_pair<3>(w, s);
 }
 
+// Keys of an image of a call that brings `rows` rows of it. own: the rows have been appended without advancing the length, and count
+// too, unless they did not fit (the append left them out then, and what lies behind the length is nobody's).
+__device__ __forceinline__ bool rows_fit(int kv_len, int rows, int Lmax) { return kv_len >= 0 && (long)kv_len + rows <= Lmax; }
+__device__ __forceinline__ int keys_of(int kv_len, int rows, bool own, int Lmax)
+{
+    return own && rows_fit(kv_len, rows, Lmax) ? kv_len + rows : min(max(kv_len, 0), Lmax);
+}
+
 // Image of compacted row r: the largest b with cu[b] <= r (B >= 1).
 __device__ __forceinline__ int image_of(const int32_t* cu, int B, int r)
 {
@@ -79,7 +87,7 @@ nova_status nova_launch_cache4_append(nova_ctx* ctx, const nova_cache4* c, const
                                       int M, int advance, cudaStream_t st);
 
 // Attention over the cache. own_rows: the keys of image b are its kv_len[b] rows and the cu[b+1] - cu[b] behind them (appended
-// without advancing the lengths), else the kv_len[b] rows alone.
+// without advancing the lengths; an image whose rows did not fit has only the former), else the kv_len[b] rows alone.
 struct nova_cache4_attn_args {
     const nova_cache4* cache;
     const __nv_bfloat16* q;        // [M, C], row stride ldq elements

@@ -114,8 +114,7 @@ struct FewWalk {
     }
     __device__ __forceinline__ static int image_len(const FewParams& p, int b)
     {
-        const int n = max(p.kv_len[b], 0) + (p.own_rows ? max(p.cu[b + 1] - p.cu[b], 0) : 0);
-        return min(n, p.Lmax);
+        return keys_of(p.kv_len[b], p.own_rows ? max(min(p.cu[b + 1], p.M) - p.cu[b], 0) : 0, p.own_rows, p.Lmax);
     }
     // Tiles of a unit, and one more for what it costs to begin and to end one.
     __device__ __forceinline__ static int tiles(int len) { return (len + FewCfg<DH>::kTile - 1) / FewCfg<DH>::kTile + 1; }

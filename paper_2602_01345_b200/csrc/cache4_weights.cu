@@ -64,8 +64,9 @@ cache4_weights_kernel(const WeightParams p)
     pdl_launch_dependents();
     const int part = blockIdx.x % p.parts, bt = blockIdx.x / p.parts, tile = bt % p.tiles, b = bt / p.tiles;
     const int c0 = p.cu[b], rows = min(max(p.cu[b + 1] - c0, 0), max(p.M - c0, 0));
-    const int len = min(max(p.kv_len[b], 0) + (p.own_rows ? rows : 0), p.Lmax);
+    const int kv_len = p.kv_len[b], len = keys_of(kv_len, rows, p.own_rows, p.Lmax);
     if (tile * kWtTile >= len) return;
+    if (p.own_rows && !rows_fit(kv_len, rows, p.Lmax)) return;      // the image's call is refused: its weights stay, for the call that repeats it
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int chunks = (rows + kWtChunk - 1) / kWtChunk, jobs = p.n_heads * chunks;
     const int j0 = (int)((long)jobs * part / p.parts), j1 = (int)((long)jobs * (part + 1) / p.parts);

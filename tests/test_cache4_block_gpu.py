@@ -256,3 +256,60 @@ def test_generation_refuses_what_does_not_go_together():
                dict(cache_bits=4, cache_budget=5, cache_recent=6)):
         with pytest.raises(AssertionError):
             pipeline.MultiScaleRunner(ctx, weights, 1, 1, (1, 2), **kw)
+
+
+@pytest.mark.parametrize("C,heads,N,ks,lens,Lmax", [(128, 2, 10, [10, 4], [20, 25], 30), (256, 2, 40, [40, 33, 17], [480, 90, 0], 520),
+                                                     (128, 1, 300, [290, 300, 2], [20, 300, 598], 600), (256, 2, 300, [300, 280], [0, 360], 640)])
+@pytest.mark.parametrize("refused", [0, 1])
+def test_block_leaves_an_image_that_overflows_as_it_was(C, heads, N, ks, lens, Lmax, refused):
+    """Its rows past kv_len hold codes of all kinds and scales of NaN: its queries attend to the rows that it has, its weights, rows and length stay, and the
+    other images get what they get in a call in which nothing overflows."""
+    ctx = nova.Context(0)
+    B, M = len(ks), sum(ks)
+    lens = list(lens)
+    lens[refused] = Lmax - ks[refused] + 1
+    wt, x, idx, cache, kv = _case(C, heads, B, N, ks, lens, Lmax, 6)
+    nova.nova_cache4_append(ctx, cache, kv[0], kv[1], _cu(lens))
+    fits = nova.Cache4.empty(B, Lmax, C, heads)       # the same rows, but for the last one of the image that is too long
+    for a, b in zip((cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales), (fits.k_codes, fits.v_codes, fits.k_scales, fits.v_scales)):
+        b.copy_(a)
+    fits.kv_len.copy_(cache.kv_len)
+    fits.kv_len[refused] -= 1
+    shape = nova.BlockShape(B, N, C, heads, 2 * C, Lmax, M)
+    ctx.ensure_block_cache4_workspace(shape)
+    runs = []
+    k_old, v_old = _read(ctx, cache, lens)
+    for c in (cache, fits):
+        before = [t.clone() for t in (c.k_codes, c.v_codes, c.k_scales.view(torch.int16), c.v_scales.view(torch.int16))]
+        weight = torch.zeros((B, Lmax), device=DEV)
+        for b in range(B):
+            weight[b, :int(c.kv_len[b])] = 0.5
+        y = torch.empty((M, C), dtype=torch.bfloat16, device=DEV)
+        nova.nova_pruned_block_forward_cache4(ctx, wt, shape, x, idx, _cu(ks), c, True, y, weight=weight)
+        assert ctx.device_status() == (2 if c is cache else 0)
+        runs.append((y, weight, before))
+    (y, weight, before), (y_fits, weight_fits, _) = runs
+    at = np.concatenate([[0], np.cumsum(ks)])
+    own = slice(at[refused], at[refused + 1])
+    n = lens[refused]
+    assert cache.kv_len.tolist() == [a + (k if b != refused else 0) for b, (a, k) in enumerate(zip(lens, ks))]
+    assert (weight[refused, :n] == 0.5).all() and (weight[refused, n:] == 0).all()
+    for t, old in zip((cache.k_codes, cache.v_codes, cache.k_scales.view(torch.int16), cache.v_scales.view(torch.int16)), before):
+        assert torch.equal(t[refused], old[refused])
+    o0 = sum(lens[:refused])
+    none = torch.empty((0, C), dtype=torch.float64)
+    ref, _ = _block64(wt, x[refused, idx[own].long()], k_old[o0:o0 + n], v_old[o0:o0 + n], none, none, heads)
+    if n:
+        assert (y[own].double().cpu() - ref).abs().max() <= 2e-2 * ref.abs().max()
+    assert torch.isfinite(y.float()).all()
+    for b in range(B):
+        if b == refused:
+            continue
+        a, z = at[b], at[b + 1]
+        # other images' sums may be cut into other parts: as in the test of the block
+        if ks[b]:
+            assert (y[a:z].double() - y_fits[a:z].double()).abs().max() <= 2e-2 * y_fits[a:z].double().abs().max()
+        assert (weight[b] - weight_fits[b]).abs().max() <= 2.0 ** -10 * weight_fits[b].abs().max()
+        assert (weight[b, lens[b] + ks[b]:] == 0).all()
+        assert torch.equal(cache.k_codes[b, :lens[b] + ks[b]], fits.k_codes[b, :lens[b] + ks[b]])
+        assert torch.equal(cache.v_codes[b, :lens[b] + ks[b]], fits.v_codes[b, :lens[b] + ks[b]])
