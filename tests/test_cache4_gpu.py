@@ -720,3 +720,30 @@ def test_attention_ranges_far_apart_share_a_row(ctx, C, rows, depth, low_first):
 def test_attention_long_cache_scores_far_apart(ctx, C, rows, q_scale):
     """157 tiles shared by up to 26 CTAs, with scores of hundreds: the ranges' references lie far apart, and items are run again."""
     _check_attention(ctx, [20011], [rows], C, 1, seed=31, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("C,heads,rows", [(128, 2, 3), (128, 1, 70), (256, 2, 200)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 3e38])
+def test_weights_of_queries_that_count_for_nothing(ctx, C, heads, rows, bad):
+    """A query whose log-sum-exp is -inf adds nothing, whatever it holds, and not to a key that is NaN either."""
+    n = 700
+    cache, k, _ = _filled(ctx, [n], n + 20, C, heads, 1)
+    q = _rows(2, rows, C).to(DEV)
+    ctx.ensure_cache4_workspace(cache, rows)
+    lse = torch.zeros((heads, rows), device=DEV)
+    o = torch.empty_like(q)
+    nova.nova_cache4_attention(ctx, cache, q, _cu([rows]), o, lse=lse)
+    dead = list(range(1, rows, 3)) + [rows - 1]
+    keep = [r for r in range(rows) if r not in dead]
+    q_dead, lse_dead = q.clone(), lse.clone()
+    q_dead[dead] = bad
+    lse_dead[:, dead] = -math.inf
+    out, two = (torch.zeros((1, n + 20), device=DEV) for _ in range(2))
+    nova.nova_cache4_weights(ctx, cache, q_dead, lse_dead, _cu([rows]), out)
+    nova.nova_cache4_weights(ctx, cache, q[keep].contiguous(), lse[:, keep].contiguous(), _cu([len(keep)]), two)
+    # the same terms, all positive, in another order: at most rows * heads additions in each sum
+    assert torch.allclose(out, two, rtol=2 * rows * heads * 2.0 ** -24, atol=0)
+    cache.k_scales[0, 5] = float("nan")
+    lse_dead.fill_(-math.inf)
+    nova.nova_cache4_weights(ctx, cache, q_dead, lse_dead, _cu([rows]), out)
+    assert (out == 0).all() and ctx.device_status() == 0
