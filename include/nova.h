@@ -34,7 +34,8 @@
  *    nova_destroy leave the caller's current device as they found it.
  *  - Device-side waits are bounded. If one expires the kernel records
  *    NOVA_ERR_TIMEOUT in the context's device status word and returns; non-finite
- *    logits record NOVA_ERR_NONFINITE. nova_device_status() reads that word.
+ *    logits, and keys or values that a 4-bit cache cannot hold, record NOVA_ERR_NONFINITE.
+ *    nova_device_status() reads that word.
  */
 #ifndef NOVA_H
 #define NOVA_H
@@ -54,7 +55,8 @@ typedef enum nova_status {
     NOVA_ERR_SHAPE = 2,        /* size outside what the kernels support             */
     NOVA_ERR_ALIGNMENT = 3,    /* pointer or stride not 16-byte aligned             */
     NOVA_ERR_WORKSPACE = 4,    /* workspace missing or too small                    */
-    NOVA_ERR_NONFINITE = 5,    /* +inf or NaN logit seen (device status)            */
+    NOVA_ERR_NONFINITE = 5,    /* +inf or NaN logit, or a key or value that a 4-bit
+                                  cache cannot hold (device status)               */
     NOVA_ERR_TIMEOUT = 6,      /* a bounded device-side wait expired (device status)*/
     NOVA_ERR_CUDA = 7          /* a CUDA runtime/driver call failed                 */
 } nova_status;
@@ -559,8 +561,8 @@ nova_status nova_restore_from_cache_device(nova_ctx* ctx, const void* x_in, cons
  * channels c..c+7 in a little-endian 32-bit word: channel c+2i in bits 4i..4i+3, channel c+2i+1 in bits 16+4i..19+4i.
  * A group that holds a NaN, an infinity or a magnitude of 2^120 or more gets scale NaN (its channels read as NaN; the
  * device status is NOVA_ERR_NONFINITE); no scale is below 2^-120 except that of zeros, which is 0.
- * C a multiple of 64, head size 64 or 128, as many K/V heads as query heads. Rows at or past kv_len[b] are never read and may
- * hold anything. Calls that take compacted rows get them as nova_select_topk writes them: image b's are cu[b] .. cu[b+1]-1 of
+ * C a multiple of 64, head size 64 or 128, as many K/V heads as query heads. Rows at or past kv_len[b] may hold anything: only
+ * nova_cache4_read, asked for them by number, reads them. Calls that take compacted rows get them as nova_select_topk writes them: image b's are cu[b] .. cu[b+1]-1 of
  * M (an upper bound of cu[B]; rows past cu[B] are neither read nor written), with a row stride of ld elements (ld >= C, a
  * multiple of 8). In debug mode cu is validated on the device first.
  */

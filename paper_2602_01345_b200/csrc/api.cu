@@ -15,7 +15,7 @@ const char* nova_status_string(nova_status s)
         case NOVA_ERR_SHAPE: return "unsupported shape";
         case NOVA_ERR_ALIGNMENT: return "misaligned pointer or stride";
         case NOVA_ERR_WORKSPACE: return "workspace missing or too small";
-        case NOVA_ERR_NONFINITE: return "non-finite logit";
+        case NOVA_ERR_NONFINITE: return "non-finite logit, or key or value that 4 bits cannot hold";
         case NOVA_ERR_TIMEOUT: return "device-side wait expired";
         case NOVA_ERR_CUDA: return "CUDA error";
     }
@@ -157,7 +157,7 @@ nova_status nova_device_status(nova_ctx* ctx, void* stream)
     if (word & NOVA_DEV_TIMEOUT) return nova_fail(ctx, NOVA_ERR_TIMEOUT, "a device-side wait expired");
     if (word & NOVA_DEV_BAD_INDEX) return nova_fail(ctx, NOVA_ERR_INVALID_ARG, "an index list failed the debug mode's validation");
     if (word & NOVA_DEV_SHAPE) return nova_fail(ctx, NOVA_ERR_SHAPE, "K/V cache overflow on the device");
-    if (word & NOVA_DEV_NONFINITE) return nova_fail(ctx, NOVA_ERR_NONFINITE, "non-finite logit");
+    if (word & NOVA_DEV_NONFINITE) return nova_fail(ctx, NOVA_ERR_NONFINITE, "a non-finite logit, or a key or value that a cache in 4 bits cannot hold");
     return NOVA_OK;
 }
 

@@ -47,7 +47,7 @@
 // result; and at head size 128 up to 128 rows per image go to CTAs alone, with two stages of whole tiles (64 rows x 29414 keys,
 // 16 heads: pairs 84 us, alone 67, 64 with the merge's loads unrolled).
 // What bounds it: the schedulers, which the decoding shares with the softmax at 80 registers a thread (61 % of the issue slots in use), and
-// the hand-overs between them: 3277 rows x 29414 keys 851 us back to back, 770 after a pause, where the bf16 cache takes 572. Measured and not
+// the hand-overs between them: 3277 rows x 29414 keys 857 us back to back, 770 after a pause, where the bf16 cache takes 572. Measured and not
 // kept: both softmax warpgroups on halves of every tile 918 us against 760; registers moved between the warpgroups (setmaxnreg) 768;
 // four stages, or a shorter ring, +-1 %.
 #include "cache4.cuh"
@@ -62,7 +62,7 @@ constexpr int BQ = 128;        // query rows per CTA
 constexpr int BKV = 128;       // keys per tile
 constexpr int kBufs = 3;       // S buffers in tensor memory
 constexpr int kThreads512 = 512;  // warpgroups: producer + issuer (+2 idle warps), epilogue, softmax 0, softmax 1
-constexpr int kThreads4 = 768; // and, with a cache in 4 bits, one that decodes keys and one that decodes values
+constexpr int kThreads4 = 768; // and, with a cache in 4 bits, two that decode, in turn
 constexpr int kSlabBytes = 128 * 128;   // [128 rows][64 bf16]
 // The probability of a score equal to the reference is 2^-kHeadroom. A row's sum of probabilities over one key tile at
 // or above kHugeSum (or NaN) means a score about 2^(80 + kHeadroom) above the reference. That is far below

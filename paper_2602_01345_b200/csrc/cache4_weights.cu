@@ -2,7 +2,7 @@
 //   out[b, j] = in[b, j] + sum over heads and queries of exp(s - lse),  s = q k_j / sqrt(dh),
 // lse being the row's log-sum-exp as the attention left it.
 //
-// A warp has 32 keys of one head as the A operand of mma.sync, decoded once into registers, and takes the image's queries, 32 at a
+// A warp has 32 keys of one head as the A operand of mma.sync, decoded once into registers, and takes the image's queries, 64 at a
 // time from shared memory, as the B operand: a thread's results then belong to two keys per tile, and the sum over
 // queries and heads stays in its registers until the end. A CTA's eight warps share the queries. What bounds it: with many
 // queries the tensor work (mma.sync) and the exponentials, one per key, query and head; with few the bytes of the keys, for

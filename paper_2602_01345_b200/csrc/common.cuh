@@ -27,7 +27,8 @@
 #define NOVA_ATTN_TICKETS 96
 #define NOVA_MEAN_MAX_CTAS 192        // the accumulator's arrival count has 8 bits
 #define NOVA_MEAN_MAX_SEGMENTS 256
-#define NOVA_TICKETS 1024             // of rows that several CTAs share: head, eight for each CTA pair (its reading warps), or attention mass, one for each CTA
+#define NOVA_TICKETS 1024             // of rows that several CTAs share: head, eight for each CTA pair (its reading warps), or attention mass, one for each CTA;
+                                      // cache4: few-row attention, one for each CTA, weights, one for each 256 keys of an image
 #define NOVA_TICKET_WORD0 (NOVA_STATUS_WORDS + NOVA_MEAN_MAX_SEGMENTS * 2)
 #define NOVA_APPEND_TICKET_WORD 4     // blocks of a cache4 append that have read the lengths
 #define NOVA_STATUS_BYTES (NOVA_STATUS_WORDS * 4 + NOVA_MEAN_MAX_SEGMENTS * 8 + NOVA_TICKETS * 4)

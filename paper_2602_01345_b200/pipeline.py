@@ -185,7 +185,9 @@ class MultiScaleRunner:
     residual cache written at the previous scale (Eq. 15; read, resized, at the next one, Eq. 16)
     and, per image, the history of scale mean entropies that the trigger of Eq. 8-10 works on. A
     scale that is not pruned yet is simply the same call sequence with every token kept.
-    With cache_bits=4 the K/V caches hold 4 bits a channel, and cache_budget bounds their rows.
+    With cache_bits=4 the K/V caches hold 4 bits a channel, and cache_budget bounds their rows. That is for memory: a layer with a few
+    kept tokens over a long cache gets faster by it, one with many gets slower (2048 channels, us a block with bf16, 4 bits, and 4 bits with
+    the weights that a budget needs: 13 rows x 10521 keys 127, 91, 116; 64 x 29300 230, 137, 189; 4 x 2048 x 6425 978, 1383, 2296).
     The backbone around the layers (token embedding, sampling) is not part of this library: the
     caller supplies each scale's layer input and logits.
     """
@@ -194,8 +196,10 @@ class MultiScaleRunner:
                  on_device: bool = False, fused_restore: bool = False, cache_bits: int = 16, cache_budget: int | None = None,
                  cache_recent: int | None = None):
         """cache_bits=4: keys and values in 4 bits (nv.Cache4), not with on_device. cache_budget, with 4 bits: after every scale each
-        layer's cache is brought back to at most this many rows per image, the last cache_recent of them (default: as many as the
-        scale has tokens) and the others with the highest attention weight so far; None keeps all rows.
+        layer's cache is brought back to at most this many rows per image, the last cache_recent of them and the others with the highest
+        attention weight so far; None keeps all rows. cache_recent defaults to as many as the scale has tokens, so that its own rows, which
+        only its own queries have weighed, all stay; behind a scale with cache_budget tokens or more nothing else does then, whatever
+        its weight. Give a smaller number to have the weights decide there.
         on_device: keep the entropy history and every keep count in device memory and run each
         scale through DeviceScaleRunner (no host synchronisation inside a scale)."""
         self.ctx, self.weights, self.n_heads, self.B, self.eps = ctx, weights, n_heads, B, eps
