@@ -313,3 +313,42 @@ def test_block_leaves_an_image_that_overflows_as_it_was(C, heads, N, ks, lens, L
         assert (weight[b, lens[b] + ks[b]:] == 0).all()
         assert torch.equal(cache.k_codes[b, :lens[b] + ks[b]], fits.k_codes[b, :lens[b] + ks[b]])
         assert torch.equal(cache.v_codes[b, :lens[b] + ks[b]], fits.v_codes[b, :lens[b] + ks[b]])
+
+
+def test_block_replays_from_a_graph():
+    """Captured on a stream of its own and replayed: each replay appends and adds weights as another eager call does."""
+    ctx = nova.Context(0)
+    C, heads, N, ks, lens, Lmax = 256, 2, 40, [40, 13], [200, 333], 500
+    wt, x, idx, cache, kv = _case(C, heads, 2, N, ks, lens, Lmax, 8)
+    nova.nova_cache4_append(ctx, cache, kv[0], kv[1], _cu(lens))
+    shape = nova.BlockShape(2, N, C, heads, 2 * C, Lmax, sum(ks))
+    ctx.ensure_block_cache4_workspace(shape)
+    weight = torch.zeros((2, Lmax), device=DEV)
+    y = torch.empty((sum(ks), C), dtype=torch.bfloat16, device=DEV)
+    cu, held = _cu(ks), (cache.k_codes, cache.v_codes, cache.k_scales, cache.v_scales, cache.kv_len, weight)
+    before = [t.clone() for t in held]
+
+    def once():
+        nova.nova_pruned_block_forward_cache4(ctx, wt, shape, x, idx, cu, cache, True, y, weight=weight)
+
+    def state():
+        n = cache.kv_len.tolist()
+        rows = [t[b, :n[b]].view(torch.uint8).clone() for t in held[:4] for b in range(2)]
+        return [n, y.clone(), weight.clone()] + rows
+
+    eager = []
+    for _ in range(3):
+        once()
+        eager.append(state())
+    for t, b in zip(held, before):
+        t.copy_(b)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        once()
+    for ref in eager:
+        graph.replay()
+        got = state()
+        assert got[0] == ref[0] and all(torch.equal(a, b) for a, b in zip(got[1:], ref[1:]))
+    assert ctx.device_status() == 0
